@@ -333,6 +333,109 @@ int hq_tensor_quantize_sr(const float *X, size_t n, const hq_range *r, uint64_t 
 int hq_tensor_quantize_dynamic(int32_t mode, const float *X, size_t n, hq_range *r, int8_t *Q,
                                hq_qparams *q_out, hq_stats *st, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Microscaled 4-bit matrices (MX4): 4-bit codes E2M1 (sign, magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ * with one E8M0 scale for every 32 values along the axis a product sums over.  No range has to be
+ * known beforehand, so there is no range state and there are no statistics: the counterpart of
+ * the 8-bit path above for layers whose operands are quantized block by block.
+ *
+ * A container holds a matrix of `rows` rows whose axis of `n` values is cut into chunks of 256
+ * (8 blocks of 32):
+ *   Q  codes   [chunks][rows][128 bytes]  two to a byte, the even element in the low half; bit 3 = sign
+ *   S  scales  [chunks][rows][8 bytes]    scale 2^(byte - 127); 255: every value of the block is NaN
+ * chunks = hq_mx4_chunks(n, 1); what lies behind the axis' end in its last chunk has code 0.  Q takes
+ * 128 and S 8 bytes per chunk and row.  Matrices of one shape follow each other, container behind
+ * container (the weights of experts).  An axis made of ragged segments (rows sorted by expert) gives
+ * every segment whole chunks of its own, segment behind segment; hq_mx4_chunks(n, segments) is the
+ * most chunks this can take, and the chunks that are left over are neither written nor read.
+ *
+ * offs (device, int32 [segments + 1]): segment e is offs[e] .. offs[e + 1] - 1, ascending within
+ * 0 .. n.  Rows before offs[0] and from offs[segments] on belong to no segment: they are not read,
+ * and what an entry point would write for them is left as it was.  (The library cannot refuse values on the
+ * device: they are clamped to 0 .. n and a descending pair is an empty segment.)
+ *
+ * Q, S, X and out are 16-byte aligned; types of real-valued tensors are HQ_FP32, HQ_BF16, HQ_FP16.
+ * ------------------------------------------------------------------------------------------- */
+#define HQ_FP32 0
+#define HQ_BF16 1
+#define HQ_FP16 2
+
+#define HQ_MX4_BLOCK 32
+#define HQ_MX4_CHUNK 256
+#define HQ_MX4_MAX_SEGMENTS 4096
+
+/* Chunks of an axis of n >= 0 values in at most `segments` >= 1 ragged segments (host, pure; 0 for
+ * arguments outside these limits):
+ * the most that any distribution of the values over the segments needs. */
+int64_t hq_mx4_chunks(int64_t n, int32_t segments);
+
+/* Quantizes a real-valued matrix into containers along its rows, along its columns, or both in one
+ * reading of X: a layer's forward product sums over one axis of a tensor, its gradients over the other.
+ *   X      [rows][cols] of type xtype; offs == NULL: `batch` >= 1 such matrices [batch][rows][cols]
+ *   Q, S   along the rows: containers of `rows` rows, axis cols (NULL, both, to skip)
+ *   Qt, St along the columns: containers of `cols` rows, axis rows (NULL, both, to skip)
+ *   offs   NULL, or: batch = number of segments, X is one matrix whose rows are sorted by segment; along
+ *          the columns every segment has chunks of its own, along the rows nothing changes (one
+ *          container).  Only rows of a segment are quantized.
+ * Per block, amax = largest magnitude: scale 2^(floor(log2 amax) - 2), not below 2^-127 (byte 0, also for an all-zero block);
+ * codes = x / scale to nearest, ties to the even code, magnitudes above 6 to 6.  A block with an infinity or a
+ * NaN gets scale byte 255 and codes 0.  rows may be 0 (nothing is launched).
+ * chunks(cols) * chunks(rows) * batch stays below 2^31, cols and rows below 2^31 - 256.                         */
+int hq_mx4_quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
+                    uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream);
+
+/* hq_mx4_quantize with stochastic rounding, unbiased: the scale is the smallest power of two that leaves
+ * no magnitude above 6 (twice the one above if amax / 2^floor(log2 amax) > 1.5), and |x| / scale goes to the
+ * grid value above it with probability of its share of the step between its neighbours: up iff that share
+ * exceeds r / 2^24, the draw as in hq_gemm_dgrad_sr with the element's linear index in X as the counter, the
+ * same draw along the rows and along the columns.                                               */
+int hq_mx4_quantize_sr(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
+                       uint64_t seed, uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream);
+
+/* The values of containers of `rows` rows and axis n, rounded to xtype once (exact but for overflow in HQ_FP16 and
+ * for values below the type's smallest):
+ *   offs == NULL: `batch` >= 1 containers -> X [batch][rows][n]
+ *   otherwise     one matrix of `batch` ragged segments along the axis -> X [rows][n]              */
+int hq_mx4_dequantize(const uint8_t *Q, const uint8_t *S, int32_t rows, int32_t n, int32_t batch, const int32_t *offs,
+                      int32_t xtype, void *X, void *stream);
+
+/* Shape of a product (host struct): out [M][N] = sum over K, of type out_type, fp32 accumulation, rounded once.
+ * M, N, K >= 0 (K = 0: out = 0; M = 0 or N = 0: nothing to do), below 2^31 - 256.                */
+typedef struct {
+    int32_t M, N, K;
+    int32_t experts;          /* 1 for hq_mx4_gemm; 1 .. HQ_MX4_MAX_SEGMENTS for the products by expert */
+    int32_t out_type;
+} hq_mx4_problem;
+
+/* Bytes of device workspace (host, pure; 0 = none, also for an invalid problem).                 */
+#define HQ_ENTRY_MX4_GEMM 5
+#define HQ_ENTRY_MX4_WGRAD_GROUPED 6
+size_t hq_mx4_workspace_bytes(int32_t entry, const hq_mx4_problem *p /* host */);
+
+/* out[m][n] = sum_k A[m][k] B[n][k], both operands containers along K: the forward pass (A = X, B = W), the
+ * input gradient (A = dY, B = W along its columns) and the weight gradient (A = dY, B = X, both along
+ * their columns) of a linear layer; M from a single row on.
+ *   ws  >= hq_mx4_workspace_bytes(HQ_ENTRY_MX4_GEMM, p) bytes, 16-byte aligned; scratch            */
+int hq_mx4_gemm(const hq_mx4_problem *p /* host */, const uint8_t *A, const uint8_t *As, const uint8_t *B, const uint8_t *Bs,
+                void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Products grouped by expert: rows sorted by expert (offs), each times its expert's matrix,
+ *   out[r][n] = sum_k A[r][k] B[e][n][k]  for offs[e] <= r < offs[e + 1].
+ *   A   one container of p->M rows along K (all experts' rows)
+ *   B   p->experts containers of N rows along K: hq_mx4_quantize of W [experts][N][K] along the rows for the
+ *       forward pass, along the columns (N and K swapped) for the input gradient
+ * Rows of no expert are left as they were.                                                       */
+int hq_mx4_gemm_grouped(const hq_mx4_problem *p /* host */, const uint8_t *A, const uint8_t *As, const uint8_t *B,
+                        const uint8_t *Bs, const int32_t *offs, void *out, void *stream);
+
+/* Weight gradients by expert: out[e][m][n] = sum over the rows r of expert e of A[m][r] B[n][r].
+ *   A, B  containers of M and N rows along the p->K rows of the batch in p->experts segments (offs):
+ *         hq_mx4_quantize of dY and X along their columns with the same offs
+ *   out   [experts][M][N]; an expert without rows gets zeros
+ *   ws    >= hq_mx4_workspace_bytes(HQ_ENTRY_MX4_WGRAD_GROUPED, p) bytes, 16-byte aligned; scratch   */
+int hq_mx4_wgrad_grouped(const hq_mx4_problem *p /* host */, const uint8_t *A, const uint8_t *As, const uint8_t *B,
+                         const uint8_t *Bs, const int32_t *offs, void *out, void *ws, size_t ws_bytes, void *stream);
+
 /* Measurement aid, not part of the method: launches a kernel in which every wavefront issues
  * iters * 8 int8 MFMAs (32x32x32, operands and accumulators in registers, no memory traffic
  * except one 4-byte store per lane to sink [blocks * 256] at the end).  Timed by the caller, it

@@ -17,6 +17,9 @@ HQ_LINEAR, HQ_CONV2D, HQ_DEPTHWISE = 0, 1, 2
 HQ_ENTRY_FWD, HQ_ENTRY_DGRAD, HQ_ENTRY_WGRAD, HQ_ENTRY_DYNAMIC_FWD, HQ_ENTRY_DYNAMIC_DGRAD = 0, 1, 2, 3, 4
 HQ_DYN_CURRENT, HQ_DYN_RUNNING = 0, 1
 HQ_STATIC_SCRATCH_BYTES = 64 << 20
+HQ_FP32, HQ_BF16, HQ_FP16 = 0, 1, 2
+HQ_MX4_BLOCK, HQ_MX4_CHUNK, HQ_MX4_MAX_SEGMENTS = 32, 256, 4096
+HQ_ENTRY_MX4_GEMM, HQ_ENTRY_MX4_WGRAD_GROUPED = 5, 6
 
 # Host views of the device structs (little-endian, same field order as include/hq.h).
 QPARAMS = np.dtype([("scale", "<f4"), ("zero_point", "<i4")])
@@ -41,6 +44,10 @@ class hq_problem(C.Structure):
                 (self.W + 2 * self.pad - self.S) // self.stride + 1)
 
 
+class hq_mx4_problem(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "N", "K", "experts", "out_type")]
+
+
 class HqError(RuntimeError):
     def __init__(self, fn, code):
         self.code = code
@@ -51,6 +58,8 @@ _lib = None
 EXPORTS = ("hq_workspace_bytes", "hq_gemm_fwd", "hq_gemm_dgrad", "hq_gemm_dgrad_sr", "hq_gemm_wgrad", "hq_gemm_wgrad_static", "hq_gemm_wgrad_update", "hq_range_update",
            "hq_range_update_batch", "hq_range_update_saturation",
            "hq_gemm_dynamic", "hq_gemm_dynamic_sr", "hq_stats_reset", "hq_stats_fold", "hq_weight_prepare", "hq_weight_quantize", "hq_tensor_quantize", "hq_tensor_quantize_sr", "hq_tensor_quantize_dynamic",
+           "hq_mx4_chunks", "hq_mx4_workspace_bytes", "hq_mx4_quantize", "hq_mx4_quantize_sr", "hq_mx4_dequantize", "hq_mx4_gemm",
+           "hq_mx4_gemm_grouped", "hq_mx4_wgrad_grouped",
            "hq_probe_mfma_rate",
            "hq_error_string")
 
@@ -87,8 +96,19 @@ def lib():
         L.hq_tensor_quantize.argtypes = [vp, C.c_size_t, vp, vp, vp, vp, vp]
         L.hq_tensor_quantize_sr.argtypes = [vp, C.c_size_t, vp, C.c_uint64, vp, vp, vp, vp]
         L.hq_tensor_quantize_dynamic.argtypes = [C.c_int32, vp, C.c_size_t, vp, vp, vp, vp, vp]
+        MP = C.POINTER(hq_mx4_problem)
+        L.hq_mx4_chunks.argtypes = [C.c_int64, C.c_int32]
+        L.hq_mx4_workspace_bytes.argtypes = [C.c_int32, MP]
+        L.hq_mx4_quantize.argtypes = [C.c_int32, vp] + [C.c_int32] * 3 + [vp] * 6
+        L.hq_mx4_quantize_sr.argtypes = [C.c_int32, vp] + [C.c_int32] * 3 + [vp, C.c_uint64] + [vp] * 5
+        L.hq_mx4_dequantize.argtypes = [vp, vp] + [C.c_int32] * 3 + [vp, C.c_int32, vp, vp]
+        L.hq_mx4_gemm.argtypes = [MP] + [vp] * 6 + [C.c_size_t, vp]
+        L.hq_mx4_gemm_grouped.argtypes = [MP] + [vp] * 7
+        L.hq_mx4_wgrad_grouped.argtypes = [MP] + [vp] * 7 + [C.c_size_t, vp]
         for f in EXPORTS[1:-1]:
             getattr(L, f).restype = C.c_int
+        L.hq_mx4_chunks.restype = C.c_int64
+        L.hq_mx4_workspace_bytes.restype = C.c_size_t
         _lib = L
     return _lib
 
@@ -215,6 +235,44 @@ def hq_tensor_quantize_dynamic(mode, X, n, r, Q, q_out, st, stream=None):
                                                                           _ptr(q_out), _ptr(st), _stream(stream)))
 
 
+def hq_mx4_chunks(n, segments=1):
+    return int(lib().hq_mx4_chunks(n, segments))
+
+
+def hq_mx4_workspace_bytes(entry, p):
+    return int(lib().hq_mx4_workspace_bytes(entry, C.byref(p)))
+
+
+def hq_mx4_quantize(xtype, X, rows, cols, batch, offs, Q, S, Qt, St, stream=None):
+    _check("hq_mx4_quantize", lib().hq_mx4_quantize(xtype, _ptr(X), rows, cols, batch, _ptr(offs), _ptr(Q), _ptr(S), _ptr(Qt),
+                                                    _ptr(St), _stream(stream)))
+
+
+def hq_mx4_quantize_sr(xtype, X, rows, cols, batch, offs, seed, Q, S, Qt, St, stream=None):
+    _check("hq_mx4_quantize_sr", lib().hq_mx4_quantize_sr(xtype, _ptr(X), rows, cols, batch, _ptr(offs), int(seed), _ptr(Q),
+                                                          _ptr(S), _ptr(Qt), _ptr(St), _stream(stream)))
+
+
+def hq_mx4_dequantize(Q, S, rows, n, batch, offs, xtype, X, stream=None):
+    _check("hq_mx4_dequantize", lib().hq_mx4_dequantize(_ptr(Q), _ptr(S), rows, n, batch, _ptr(offs), xtype, _ptr(X),
+                                                        _stream(stream)))
+
+
+def hq_mx4_gemm(p, A, As, B, Bs, out, ws, ws_bytes, stream=None):
+    _check("hq_mx4_gemm", lib().hq_mx4_gemm(C.byref(p), _ptr(A), _ptr(As), _ptr(B), _ptr(Bs), _ptr(out), _ptr(ws), ws_bytes,
+                                            _stream(stream)))
+
+
+def hq_mx4_gemm_grouped(p, A, As, B, Bs, offs, out, stream=None):
+    _check("hq_mx4_gemm_grouped", lib().hq_mx4_gemm_grouped(C.byref(p), _ptr(A), _ptr(As), _ptr(B), _ptr(Bs), _ptr(offs),
+                                                            _ptr(out), _stream(stream)))
+
+
+def hq_mx4_wgrad_grouped(p, A, As, B, Bs, offs, out, ws, ws_bytes, stream=None):
+    _check("hq_mx4_wgrad_grouped", lib().hq_mx4_wgrad_grouped(C.byref(p), _ptr(A), _ptr(As), _ptr(B), _ptr(Bs), _ptr(offs),
+                                                              _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
 def hq_probe_mfma_rate(blocks, iters, sink, stream=None):
     """Launches the register-only MFMA loop; returns the int8 operations it issues."""
     _check("hq_probe_mfma_rate", lib().hq_probe_mfma_rate(blocks, iters, _ptr(sink), _stream(stream)))
@@ -227,6 +285,27 @@ def hq_probe_mfma_rate(blocks, iters, sink, stream=None):
 
 def problem(kind, B, H, W, Cin, R, S, stride, pad, Cout):
     return hq_problem(kind, B, H, W, Cin, R, S, stride, pad, Cout)
+
+
+def mx4_problem(M, N, K, experts=1, out_type=HQ_FP32):
+    return hq_mx4_problem(M, N, K, experts, out_type)
+
+
+def mx4_type(dtype):
+    """HQ_FP32, HQ_BF16 or HQ_FP16 of a torch dtype."""
+    types = {"torch.float32": HQ_FP32, "torch.bfloat16": HQ_BF16, "torch.float16": HQ_FP16}
+    if str(dtype) not in types:
+        raise ValueError("MX4 takes torch.float32, bfloat16 and float16, not %s" % dtype)
+    return types[str(dtype)]
+
+
+def new_mx4(rows, n, segments=1, batch=1, device="cuda"):
+    """(codes, scales): uninitialised containers of `batch` matrices of `rows` rows and an axis of n values in ragged segments
+    (0 or 1: one)."""
+    import torch
+    chunks = batch * hq_mx4_chunks(n, max(1, segments))
+    return (torch.empty((chunks, rows, HQ_MX4_CHUNK // 2), dtype=torch.uint8, device=device),
+            torch.empty((chunks, rows, HQ_MX4_CHUNK // HQ_MX4_BLOCK), dtype=torch.uint8, device=device))
 
 
 def to_device(rec, device="cuda"):

@@ -318,6 +318,13 @@ __device__ inline void hq_lds_load16(const int8_t *base, unsigned off, unsigned 
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
                  : "=&s"(keep) : "v"(off), "s"(base), "s"(dst) : "memory");
 }
+// ... 4 bytes per lane: lane l lands at dst + 4 * l.
+__device__ inline void hq_lds_load4(const void *base, unsigned off, unsigned dst)
+{
+    unsigned keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep) : "v"(off), "s"(base), "s"(dst) : "memory");
+}
 // ... to a pointer that is the same in all lanes.
 __device__ inline unsigned hq_lds_address(void *wave_base)
 {

@@ -1,0 +1,446 @@
+// Products of microscaled 4-bit matrices: hq_mx4_gemm, hq_mx4_gemm_grouped (ragged rows by expert), hq_mx4_wgrad_grouped
+// (ragged segments of the contraction).
+//
+//   out[m][n] = sum_blocks 2^(sa[m][b] + sb[n][b] - 254) sum_{k in b} a[m][k] b[n][k]
+//
+// on the scaled MFMA (32 x 32 x 64, fp4 x fp4): a lane holds one block of a row, 16 bytes, and its scale byte; the products are summed
+// in fp32 by the matrix pipe.  Containers are cut along the contraction into chunks of 256 values, 128 bytes a row; the rows of a chunk
+// follow each other, so a tile's operands of one chunk are one run of memory, at any row offset, and there is no tail along the contraction
+// (behind its end the codes are 0).
+#include "hq_internal.h"
+#include "hq_mx4.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace {
+
+enum { DENSE = 0, BY_ROWS = 1, BY_CHUNKS = 2 };   // one product; rows of A by expert; chunks of both by expert
+
+struct ProductArgs {
+    const uint8_t *A, *As, *B, *Bs;
+    const int *offs;
+    void *out;
+    float *part;                   // partial sums of split contractions [splits][outputs], or NULL
+    size_t outputs;
+    int M, N;                      // rows of A and of out (BY_ROWS: of all experts together), rows of B
+    int chunks;                    // of the contraction (BY_CHUNKS: the most that the segments can have)
+    int rows;                      // BY_CHUNKS: values along the contraction in all segments
+    int experts, splits;
+    int m_tiles, n_tiles;
+    int out_type;
+};
+
+template <int SCALE_BYTE> __device__ inline v16f mfma32(v4i a, v4i b, v16f c, int sa, int sb)
+{
+    const v8i a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, SCALE_BYTE, sa, SCALE_BYTE, sb);
+}
+template <int SCALE_BYTE> __device__ inline v4f mfma16(v4i a, v4i b, v4f c, int sa, int sb)
+{
+    const v8i a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, SCALE_BYTE, sa, SCALE_BYTE, sb);
+}
+
+// Before results of mfma16 go to LDS: the compiler (clang of ROCm 7.2) stored the first ones right behind the loop that makes them, without the
+// wait states that the matrix pipe needs before its registers are read (it puts them before the second store).
+__device__ inline void mfma16_done(v4f &c) { asm volatile("s_nop 15" : "+v"(c)); }
+
+// COUNT consecutive outputs from column n on, of N, to `dst` (the address of column n); rounded once.
+template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const float *v, int n, int N)
+{
+    typedef typename HqReal<TYPE>::T T;
+    T *d = static_cast<T *>(dst);
+    if (n + COUNT <= N) {
+        T t[COUNT];
+#pragma unroll
+        for (int e = 0; e < COUNT; e++) t[e] = HqReal<TYPE>::store(v[e]);
+        __builtin_memcpy(__builtin_assume_aligned(d, sizeof(T)), t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int e = 0; e < COUNT; e++)
+            if (n + e < N) d[e] = HqReal<TYPE>::store(v[e]);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Tiles of BM x BN outputs, WM x WN wavefronts of (BM / WM) x (BN / WN) each.  A stage is one chunk of the tile's rows of A and B, straight
+// from memory into one of two LDS buffers; the 16-byte blocks of a row are XOR-swizzled by the row.
+// ---------------------------------------------------------------------------------------
+template <int BM, int BN, int WM, int WN, int GROUP>
+__global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArgs a)
+{
+    constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int CODE_LOADS = (BM + BN) / 8 / NW, SCALE_LOADS = (BM + BN) / 32 / NW;
+    static_assert(CODE_LOADS * 8 * NW == BM + BN && SCALE_LOADS * 32 * NW == BM + BN, "whole loads");
+    constexpr int STAGE = (BM + BN) * (MX_CODES + MX_SCALES);
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int half = lane >> 5, r32 = lane & 31, wm = wave / WN, wn = wave % WN;
+
+    // ---- which tile: each XCD takes a run of them, in bands of 8 row tiles
+    const int per_split = a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? a.experts : 1);
+    const int split = blockIdx.x / per_split;
+    int tile = blockIdx.x - split * per_split;
+    const int per = per_split / 8;
+    if (tile < per * 8) tile = (tile & 7) * per + (tile >> 3);
+    int e = 0;
+    if (GROUP == BY_CHUNKS) { e = tile / (a.m_tiles * a.n_tiles); tile -= e * (a.m_tiles * a.n_tiles); }
+    const int band = tile / (8 * a.n_tiles), in_band = min(8, a.m_tiles - 8 * band), rest = tile - band * 8 * a.n_tiles;
+    const int tile_n = rest / in_band, tile_m = 8 * band + rest - tile_n * in_band;
+
+    int m0 = tile_m * BM, m_end = a.M, chunk0 = 0, nst = a.chunks;
+    const int n0 = tile_n * BN;
+    size_t b_chunk0 = 0;
+    if (GROUP == BY_ROWS) {
+        const HqSegment s = hq_segment_of<BM>(a.offs, a.experts, a.M, tile_m);
+        if (s.e < 0) return;
+        m0 = s.first + s.unit * BM;
+        m_end = s.end;
+        b_chunk0 = (size_t)s.e * (size_t)a.chunks;
+    } else if (GROUP == BY_CHUNKS) {
+        const HqSegment s = hq_segment_start<MX_CHUNK>(a.offs, a.rows, e);
+        chunk0 = min(max(s.unit, 0), a.chunks);
+        nst = min((s.end - s.first + MX_CHUNK - 1) / MX_CHUNK, a.chunks - chunk0);
+    }
+    if (a.splits > 1) {
+        const int from = (int)((long)nst * split / a.splits), to = (int)((long)nst * (split + 1) / a.splits);
+        chunk0 += from;
+        nst = to - from;
+    }
+    if (GROUP != BY_ROWS) b_chunk0 = (size_t)chunk0;
+
+    // ---- loads: 8 rows of codes or 32 rows of scales each; rows past the end repeat the last (never stored)
+    const uint8_t *code_base[CODE_LOADS], *scale_base[SCALE_LOADS];
+    unsigned code_off[CODE_LOADS], scale_off[SCALE_LOADS];
+    const size_t a_row0 = (size_t)chunk0 * (size_t)a.M + (size_t)m0, b_row0 = b_chunk0 * (size_t)a.N + (size_t)n0;
+    auto row_of = [&](int row) __attribute__((always_inline)) {          // LDS row -> row of its operand, from the tile's first
+        const bool is_a = row < BM;
+        const int r = is_a ? row : ((row - BM) & ~31) + hq_sigma32((row - BM) & 31);
+        return min(r, is_a ? m_end - 1 - m0 : a.N - 1 - n0);
+    };
+#pragma unroll
+    for (int k = 0; k < CODE_LOADS; k++) {
+        const int first = 8 * (NW * k + wave), row = first + (lane >> 3);
+        code_base[k] = first < BM ? a.A + a_row0 * MX_CODES : a.B + b_row0 * MX_CODES;
+        code_off[k] = (unsigned)row_of(row) * MX_CODES + 16u * (unsigned)((lane & 7) ^ ((row >> 1) & 7));
+    }
+#pragma unroll
+    for (int k = 0; k < SCALE_LOADS; k++) {
+        const int first = 32 * (NW * k + wave), row = first + (lane >> 1);
+        scale_base[k] = first < BM ? a.As + a_row0 * MX_SCALES : a.Bs + b_row0 * MX_SCALES;
+        scale_off[k] = (unsigned)row_of(row) * MX_SCALES + 4u * (unsigned)(lane & 1);
+    }
+    const unsigned lds0 = hq_lds_address(smem);
+    auto request = [&](int buf) __attribute__((always_inline)) {         // the next stage
+        const unsigned dst = lds0 + buf * STAGE;
+#pragma unroll
+        for (int k = 0; k < CODE_LOADS; k++) {
+            hq_lds_load16(reinterpret_cast<const int8_t *>(code_base[k]), code_off[k], dst + 1024 * (NW * k + wave));
+            code_base[k] += (size_t)(8 * (NW * k + wave) < BM ? a.M : a.N) * MX_CODES;
+        }
+#pragma unroll
+        for (int k = 0; k < SCALE_LOADS; k++) {
+            hq_lds_load4(scale_base[k], scale_off[k], dst + (BM + BN) * MX_CODES + 256 * (NW * k + wave));
+            scale_base[k] += (size_t)(32 * (NW * k + wave) < BM ? a.M : a.N) * MX_SCALES;
+        }
+    };
+
+    v16f acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) acc[i][j][k] = 0.0f;
+
+    v4i fa[2][TM], fb[2][TN];
+    int sa[TM], sb[TN];
+    const int row_a = wm * (BM / WM) + r32, row_b = BM + wn * (BN / WN) + r32;
+    auto scales = [&](int buf) __attribute__((always_inline)) {
+        const uint8_t *p = smem + buf * STAGE + (BM + BN) * MX_CODES + 4 * half;
+#pragma unroll
+        for (int i = 0; i < TM; i++) sa[i] = *reinterpret_cast<const int *>(p + (row_a + 32 * i) * MX_SCALES);
+#pragma unroll
+        for (int j = 0; j < TN; j++) sb[j] = *reinterpret_cast<const int *>(p + (row_b + 32 * j) * MX_SCALES);
+    };
+    auto fragments = [&](int buf, int step) __attribute__((always_inline)) {
+        const uint8_t *p = smem + buf * STAGE + 16 * ((4 * half + step) ^ ((r32 >> 1) & 7));
+#pragma unroll
+        for (int i = 0; i < TM; i++) fa[step & 1][i] = *reinterpret_cast<const v4i *>(p + (row_a + 32 * i) * MX_CODES);
+#pragma unroll
+        for (int j = 0; j < TN; j++) fb[step & 1][j] = *reinterpret_cast<const v4i *>(p + (row_b + 32 * j) * MX_CODES);
+    };
+
+    if (nst > 0) request(0);
+    if (nst > 1) { request(1); asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CODE_LOADS + SCALE_LOADS) : "memory"); }
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (nst > 0) { scales(0); fragments(0, 0); }
+    int cur = 0;
+    for (int s = 0; s < nst; s++) {
+        auto multiply = [&](auto step, const int *qa, const int *qb) __attribute__((always_inline)) {
+            constexpr int K = decltype(step)::value;
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+#pragma unroll
+                for (int j = 0; j < TN; j++) acc[i][j] = mfma32<K>(fb[K & 1][j], fa[K & 1][i], acc[i][j], qb[j], qa[i]);
+        };
+        fragments(cur, 1);
+        multiply(std::integral_constant<int, 0>(), sa, sb);
+        fragments(cur, 2);
+        multiply(std::integral_constant<int, 1>(), sa, sb);
+        fragments(cur, 3);
+        multiply(std::integral_constant<int, 2>(), sa, sb);
+        int qa[TM], qb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; i++) qa[i] = sa[i];
+#pragma unroll
+        for (int j = 0; j < TN; j++) qb[j] = sb[j];
+        if (s + 1 < nst) {
+            // all fragments of this stage are in registers at the barrier: its buffer takes the stage after next
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (s + 2 < nst) request(cur);
+            cur ^= 1;
+            scales(cur);
+            fragments(cur, 0);
+        }
+        multiply(std::integral_constant<int, 3>(), qa, qb);
+    }
+
+    // ---- 16 consecutive columns of a row per lane and 32 x 32 block
+    auto finish = [&](auto type, void *out) __attribute__((always_inline)) {
+        constexpr int TYPE = decltype(type)::value;
+        typedef typename HqReal<TYPE>::T T;
+#pragma unroll
+        for (int i = 0; i < TM; i++) {
+            const int m = m0 + wm * (BM / WM) + 32 * i + r32;
+            if (m >= m_end) continue;
+#pragma unroll
+            for (int j = 0; j < TN; j++) {
+                const int n = n0 + wn * (BN / WN) + 32 * j + 16 * half;
+                float v[16];
+#pragma unroll
+                for (int k = 0; k < 16; k++) v[k] = acc[i][j][k];
+                store_run<TYPE, 16>(static_cast<T *>(out) + ((size_t)m * (size_t)a.N + (size_t)n), v, n, a.N);
+            }
+        }
+    };
+    const size_t expert_out = GROUP == BY_CHUNKS ? (size_t)e * (size_t)a.M * (size_t)a.N : 0;
+    if (a.splits > 1) finish(std::integral_constant<int, HQ_FP32>(), a.part + (size_t)split * a.outputs + expert_out);
+    else if (a.out_type == HQ_FP32) finish(std::integral_constant<int, HQ_FP32>(), static_cast<float *>(a.out) + expert_out);
+    else if (a.out_type == HQ_BF16) finish(std::integral_constant<int, HQ_BF16>(), static_cast<unsigned short *>(a.out) + expert_out);
+    else finish(std::integral_constant<int, HQ_FP16>(), static_cast<unsigned short *>(a.out) + expert_out);
+}
+
+// ---------------------------------------------------------------------------------------
+// Few rows: the bytes of B and latency count.  A workgroup takes 16 rows of B (of one expert) and all rows of A that meet them, 16 * MT at a time;
+// its wavefronts share the chunks between them and are added in LDS.  Fragments come straight from memory, a lane 32 bytes of a row.
+// ---------------------------------------------------------------------------------------
+template <int MT, int GROUP> __global__ __launch_bounds__(512) void mx4_row_kernel(const ProductArgs a)
+{
+    __shared__ float sums[8][MT][16][17];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int r16 = lane & 15, group = lane >> 4;
+    const int e = GROUP == BY_ROWS ? blockIdx.x / a.n_tiles : 0;
+    const int n0 = (int)(blockIdx.x - (unsigned)e * (unsigned)a.n_tiles) * 16;
+    int m_first = 0, m_end = a.M;
+    if (GROUP == BY_ROWS) {
+        m_first = hq_segment_bound(a.offs, e, a.M);
+        m_end = hq_segment_bound(a.offs, e + 1, a.M);
+    }
+    const size_t n = (size_t)min(n0 + r16, a.N - 1);
+    const uint8_t *b = a.B + ((size_t)e * (size_t)a.chunks * (size_t)a.N + n) * MX_CODES + 32 * group;
+    const uint8_t *bs = a.Bs + ((size_t)e * (size_t)a.chunks * (size_t)a.N + n) * MX_SCALES + 2 * group;
+    for (int m0 = m_first; m0 < m_end; m0 += 16 * MT) {
+        v4f acc[MT];
+        size_t m[MT];
+#pragma unroll
+        for (int t = 0; t < MT; t++) {
+            acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            m[t] = (size_t)min(m0 + 16 * t + r16, m_end - 1);
+        }
+        for (int c = wave; c < a.chunks; c += waves) {
+            const uint8_t *bp = b + (size_t)c * (size_t)a.N * MX_CODES;
+            const v4i b0 = *reinterpret_cast<const v4i *>(bp), b1 = *reinterpret_cast<const v4i *>(bp + 16);
+            const int sb = *reinterpret_cast<const unsigned short *>(bs + (size_t)c * (size_t)a.N * MX_SCALES);
+#pragma unroll
+            for (int t = 0; t < MT; t++) {
+                const size_t row = (size_t)c * (size_t)a.M + m[t];
+                const uint8_t *ap = a.A + row * MX_CODES + 32 * group;
+                const v4i a0 = *reinterpret_cast<const v4i *>(ap), a1 = *reinterpret_cast<const v4i *>(ap + 16);
+                const int sa = *reinterpret_cast<const unsigned short *>(a.As + row * MX_SCALES + 2 * group);
+                acc[t] = mfma16<0>(b0, a0, acc[t], sb, sa);
+                acc[t] = mfma16<1>(b1, a1, acc[t], sb, sa);
+            }
+        }
+        // (lane: row r16 of A, rows 4 * group .. + 3 of B)
+#pragma unroll
+        for (int t = 0; t < MT; t++) mfma16_done(acc[t]);
+#pragma unroll
+        for (int t = 0; t < MT; t++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) sums[wave][t][r16][4 * group + k] = acc[t][k];
+        __syncthreads();
+        for (int k = threadIdx.x; k < MT * 256; k += blockDim.x) {
+            const int row = m0 + (k >> 4), col = n0 + (k & 15);
+            float v = 0.0f;
+            for (int w = 0; w < waves; w++) v = __fadd_rn(v, sums[w][k >> 8][(k >> 4) & 15][k & 15]);
+            if (row < m_end && col < a.N) {
+                const size_t o = (size_t)row * (size_t)a.N + (size_t)col;
+                if (a.out_type == HQ_FP32) static_cast<float *>(a.out)[o] = v;
+                else if (a.out_type == HQ_BF16) static_cast<unsigned short *>(a.out)[o] = HqReal<HQ_BF16>::store(v);
+                else static_cast<unsigned short *>(a.out)[o] = HqReal<HQ_FP16>::store(v);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---- partial sums of split contractions, added in order -----------------------------------
+template <int TYPE> __global__ __launch_bounds__(HQ_THREADS) void mx4_join_kernel(const float *part, size_t outputs, int splits, void *out)
+{
+    typedef typename HqReal<TYPE>::T T;
+    const size_t groups = (outputs + 3) / 4;
+    for (size_t g = (size_t)blockIdx.x * HQ_THREADS + threadIdx.x; g < groups; g += (size_t)gridDim.x * HQ_THREADS) {
+        const int have = (int)min((size_t)4, outputs - 4 * g);
+        float v[4] = {};
+        for (int s = 0; s < splits; s++) {
+            const float *p = part + (size_t)s * outputs + 4 * g;
+            float x[4] = {};
+            if (have == 4) __builtin_memcpy(x, __builtin_assume_aligned(p, 4), 16);
+            else
+                for (int j = 0; j < have; j++) x[j] = p[j];
+#pragma unroll
+            for (int j = 0; j < 4; j++) v[j] = __fadd_rn(v[j], x[j]);
+        }
+        store_run<TYPE, 4>(static_cast<T *>(out) + 4 * g, v, 0, have);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+inline int launch_status() { return hipGetLastError() == hipSuccess ? HQ_OK : HQ_E_HIP; }
+
+int check_product(const hq_mx4_problem *p, bool grouped)
+{
+    if (!p) return HQ_E_BADARG;
+    if (!hq_mx4_type_ok(p->out_type)) return HQ_E_BADARG;
+    if (p->M < 0 || p->N < 0 || p->K < 0 || p->M >= MX_MOST || p->N >= MX_MOST || p->K >= MX_MOST) return HQ_E_BADSHAPE;
+    if (p->experts < 1 || p->experts > (grouped ? HQ_MX4_MAX_SEGMENTS : 1)) return HQ_E_BADSHAPE;
+    return HQ_OK;
+}
+
+struct Plan { int tile, splits; };                 // tile: 0 few rows; otherwise the tile's side
+
+int tiles_of(long n, int side) { return (int)((n + side - 1) / side); }
+
+// Contractions are split where tiles alone leave compute units idle.
+Plan plan_of(const hq_mx4_problem *p, int group)
+{
+    if (group != BY_CHUNKS && p->M <= 16 * (long)p->experts) return Plan{0, 1};
+    const long tiles = (long)tiles_of(p->M, 128) * tiles_of(p->N, 128) * (group == BY_CHUNKS ? p->experts : 1);
+    int splits = 1;
+    if (group != BY_ROWS) {
+        const long chunks = hq_mx4_chunks(p->K, 1) / p->experts;
+        while (tiles * splits < 512 && chunks / (splits * 2) >= 4) splits *= 2;
+    }
+    return Plan{128, splits};
+}
+
+size_t outputs_of(const hq_mx4_problem *p, int group)
+{
+    return (size_t)p->M * (size_t)p->N * (group == BY_CHUNKS ? (size_t)p->experts : 1);
+}
+
+template <int BM, int BN, int WM, int WN, int GROUP> int launch_tile(const ProductArgs &a, long blocks, hipStream_t s)
+{
+    const size_t lds = 2 * (BM + BN) * (MX_CODES + MX_SCALES);
+    static std::atomic<unsigned long long> allowed{0};
+    if (!hq_allow_lds(mx4_tile_kernel<BM, BN, WM, WN, GROUP>, lds, allowed)) return HQ_E_HIP;
+    hipLaunchKernelGGL((mx4_tile_kernel<BM, BN, WM, WN, GROUP>), dim3((unsigned)blocks), dim3(64 * WM * WN), lds, s, a);
+    return launch_status();
+}
+
+template <int GROUP> int product(const hq_mx4_problem *p, const uint8_t *A, const uint8_t *As, const uint8_t *B, const uint8_t *Bs,
+                                 const int32_t *offs, void *out, void *ws, size_t ws_bytes, void *stream)
+{
+    int rc = check_product(p, GROUP != DENSE);
+    if (rc != HQ_OK) return rc;
+    if (misaligned(A, 16) || misaligned(As, 16) || misaligned(B, 16) || misaligned(Bs, 16) || misaligned(out, 16) || misaligned(offs, 4)) return HQ_E_BADARG;
+    if (p->M == 0 || p->N == 0) return HQ_OK;
+    if (!out || (GROUP != DENSE && !offs) || (p->K > 0 && (!A || !As || !B || !Bs))) return HQ_E_BADARG;
+    const Plan plan = plan_of(p, GROUP);
+    ProductArgs a = {};
+    a.A = A; a.As = As; a.B = B; a.Bs = Bs; a.offs = offs; a.out = out;
+    a.M = p->M; a.N = p->N; a.experts = p->experts; a.out_type = p->out_type;
+    a.chunks = (int)hq_mx4_chunks(p->K, GROUP == BY_CHUNKS ? p->experts : 1);
+    a.rows = p->K;
+    a.outputs = outputs_of(p, GROUP);
+    a.splits = plan.splits;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (plan.splits > 1) {
+        if (!ws || ws_bytes < 4 * a.outputs * plan.splits || misaligned(ws, 16)) return HQ_E_WORKSPACE;
+        a.part = static_cast<float *>(ws);
+    }
+    if constexpr (GROUP != BY_CHUNKS) {
+        if (plan.tile == 0) {
+            a.n_tiles = tiles_of(p->N, 16);
+            const long blocks = (long)a.n_tiles * p->experts;
+            if (blocks >= 0x7fffffffL) return HQ_E_BADSHAPE;
+            int waves = 1;
+            while (waves < 8 && waves < a.chunks) waves *= 2;
+            hipLaunchKernelGGL((mx4_row_kernel<1, GROUP>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
+            return launch_status();
+        }
+    }
+    const int side = plan.tile;
+    const int used = std::min(p->experts, p->M);
+    a.m_tiles = GROUP == BY_ROWS ? (p->M - used) / side + used : tiles_of(p->M, side);
+    a.n_tiles = tiles_of(p->N, side);
+    const double blocks = (double)a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? p->experts : 1) * a.splits;
+    if (blocks >= 2147483648.0) return HQ_E_BADSHAPE;
+    rc = launch_tile<128, 128, 2, 2, GROUP>(a, (long)blocks, s);
+    if (rc != HQ_OK || a.splits == 1) return rc;
+    const unsigned join = (unsigned)std::min<size_t>((a.outputs / 4 + HQ_THREADS) / HQ_THREADS, 2048);
+    switch (p->out_type) {
+    case HQ_FP32: hipLaunchKernelGGL(mx4_join_kernel<HQ_FP32>, dim3(join), dim3(HQ_THREADS), 0, s, a.part, a.outputs, a.splits, out); break;
+    case HQ_BF16: hipLaunchKernelGGL(mx4_join_kernel<HQ_BF16>, dim3(join), dim3(HQ_THREADS), 0, s, a.part, a.outputs, a.splits, out); break;
+    default:      hipLaunchKernelGGL(mx4_join_kernel<HQ_FP16>, dim3(join), dim3(HQ_THREADS), 0, s, a.part, a.outputs, a.splits, out); break;
+    }
+    return launch_status();
+}
+
+} // namespace
+
+extern "C" {
+
+size_t hq_mx4_workspace_bytes(int32_t entry, const hq_mx4_problem *p)
+{
+    if (entry != HQ_ENTRY_MX4_GEMM && entry != HQ_ENTRY_MX4_WGRAD_GROUPED) return 0;
+    const int group = entry == HQ_ENTRY_MX4_GEMM ? DENSE : BY_CHUNKS;
+    if (check_product(p, group != DENSE) != HQ_OK || p->M == 0 || p->N == 0) return 0;
+    const Plan plan = plan_of(p, group);
+    return plan.splits > 1 ? 4 * outputs_of(p, group) * (size_t)plan.splits : 0;
+}
+
+int hq_mx4_gemm(const hq_mx4_problem *p, const uint8_t *A, const uint8_t *As, const uint8_t *B, const uint8_t *Bs, void *out, void *ws,
+                size_t ws_bytes, void *stream)
+{
+    return product<DENSE>(p, A, As, B, Bs, nullptr, out, ws, ws_bytes, stream);
+}
+
+int hq_mx4_gemm_grouped(const hq_mx4_problem *p, const uint8_t *A, const uint8_t *As, const uint8_t *B, const uint8_t *Bs,
+                        const int32_t *offs, void *out, void *stream)
+{
+    return product<BY_ROWS>(p, A, As, B, Bs, offs, out, nullptr, 0, stream);
+}
+
+int hq_mx4_wgrad_grouped(const hq_mx4_problem *p, const uint8_t *A, const uint8_t *As, const uint8_t *B, const uint8_t *Bs,
+                         const int32_t *offs, void *out, void *ws, size_t ws_bytes, void *stream)
+{
+    return product<BY_CHUNKS>(p, A, As, B, Bs, offs, out, ws, ws_bytes, stream);
+}
+
+} // extern "C"

@@ -1,0 +1,402 @@
+// Microscaled 4-bit quantization (hq_mx4_quantize, hq_mx4_quantize_sr) and its inverse (hq_mx4_dequantize).
+//
+//   block of 32 values x along an axis:  byte = max(exponent field of max |x| - 2 [+ 1 if its mantissa > 1.5: stochastic], 0)
+//   t = |x| 2^(127 - byte), exact in fp32; code = t to nearest even on the grid 0 .. 6, or up with probability of t's share of its step
+//
+// Bound by HBM: 4 or 2 bytes read per value, 17/32 of a byte written per direction.  A wavefront takes 32 rows of 256 columns, four columns
+// a lane, whose values stay in registers: the 32 values of a block along the columns are one lane's own, those of a block along the
+// rows lie in eight neighbouring lanes (three DPP steps find their maximum).  Eight wavefronts make the 256 rows of a chunk along the
+// columns; its codes are put together in LDS, so that both containers are written in whole 128-byte lines.
+#include "hq_internal.h"
+#include "hq_mx4.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr int MQ_ROWS = 32;                        // rows of a wavefront
+constexpr int MQ_PITCH = MX_CODES + 16;            // LDS row of a column's codes: 8 lanes' 16-byte stores fall into different banks
+
+struct QuantizeArgs {
+    const void *X;
+    const int *offs;
+    uint8_t *Q, *S, *Qt, *St;
+    int rows, cols, segments;
+    int kc;                                        // chunks along the columns' axis (of a row)
+    int tiles;                                     // row tiles of a matrix (without offs)
+    HqSr sr;
+};
+
+// A lane's four values of one row: loaded bits, and the values.
+template <int TYPE> struct Four { typedef v2i T; };
+template <> struct Four<HQ_FP32> { typedef v4i T; };
+
+template <int TYPE> __device__ inline float four_value(const typename Four<TYPE>::T &v, int j)
+{
+    if constexpr (TYPE == HQ_FP32) return __int_as_float(v[j]);
+    else return HqReal<TYPE>::load((unsigned short)((unsigned)v[j >> 1] >> (16 * (j & 1))));
+}
+
+typedef unsigned short v2us __attribute__((ext_vector_type(2)));
+__device__ inline int pk_max_u16(int a, int b)
+{
+    return __builtin_bit_cast(int, __builtin_elementwise_max(__builtin_bit_cast(v2us, a), __builtin_bit_cast(v2us, b)));
+}
+
+// fp32 bits of a magnitude held as its type's own bits (they order like the magnitudes; infinities and NaN on top).
+template <int TYPE> __device__ inline unsigned magnitude_bits(unsigned m)
+{
+    if constexpr (TYPE == HQ_FP32) return m;
+    else return __float_as_uint(HqReal<TYPE>::load((unsigned short)m));
+}
+
+struct BlockScale {
+    int byte;
+    float unit;                                    // nearest: 2^(byte - 127); stochastic: 2^(127 - byte)
+    int mask;                                      // 0 for a block that is not finite
+};
+template <bool SR> __device__ inline BlockScale block_scale(unsigned bits)
+{
+    const bool finite = bits < 0x7f800000u;
+    int byte = (int)(bits >> 23) - 2;
+    if (SR) byte += (bits & 0x7fffffu) > 0x400000u;
+    byte = max(byte, 0);
+    BlockScale s;
+    s.byte = finite ? byte : 255;
+    if (SR) s.unit = __int_as_float(finite ? (254 - byte) << 23 : 0);
+    else    s.unit = __int_as_float(byte ? byte << 23 : 0x400000);      // (2^-127 is below the smallest normal number)
+    s.mask = finite ? -1 : 0;
+    return s;
+}
+
+// x to the grid value below or above it, in units of the block's scale; u: 24 random bits / 2^24.  (Infinities and NaN: masked by the caller.)
+__device__ inline float stochastic_value(float x, float factor, float u)
+{
+    const float t = __fmul_rn(fabsf(x), factor);
+    // steps are 0.5 below 2, 1 below 4, 2 from there on: half of the power of two below t, which counts from 1
+    const int power = max(__float_as_int(t), 0x3f800000) & 0x7f800000;
+    const float q = __fmul_rn(t, __int_as_float(0x7f800000 - power)), low = floorf(q);
+    const float v = __fmul_rn(__fsub_rn(q, low) > u ? __fadd_rn(low, 1.0f) : low, __int_as_float(power - 0x800000));
+    return copysignf(v, x);
+}
+
+template <int TYPE, bool ROWS, bool COLS, bool SR, int NW>
+__global__ __launch_bounds__(64 * NW) void mx4_quantize_kernel(const QuantizeArgs a)
+{
+    typedef typename HqReal<TYPE>::T T;
+    typedef typename Four<TYPE>::T F;
+    constexpr int TILE = MQ_ROWS * NW;
+    static_assert(!COLS || TILE == MX_CHUNK, "a workgroup makes whole chunks along the columns");
+    __shared__ __attribute__((aligned(16))) uint8_t codes[COLS ? MX_CHUNK * MQ_PITCH : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t col_scales[COLS ? MX_CHUNK * MX_SCALES : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t row_scales[ROWS ? NW * MQ_ROWS * MX_SCALES : 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned y = blockIdx.x / (unsigned)a.kc;
+    const int c = (int)(blockIdx.x - y * (unsigned)a.kc);
+
+    int r0, valid;                                 // the workgroup's rows
+    size_t matrix = 0;
+    if (a.offs) {
+        const HqSegment s = hq_segment_of<TILE>(a.offs, a.segments, a.rows, (int)y);
+        if (s.e < 0) return;                       // (the same for all wavefronts)
+        r0 = s.first + s.unit * TILE;
+        valid = min(TILE, s.end - r0);
+    } else {
+        matrix = y / (unsigned)a.tiles;
+        r0 = (int)(y - (unsigned)matrix * (unsigned)a.tiles) * TILE;
+        valid = min(TILE, a.rows - r0);
+    }
+    const int rw = r0 + MQ_ROWS * wave, vw = min(max(valid - MQ_ROWS * wave, 0), MQ_ROWS);
+    const int c0 = c * MX_CHUNK + 4 * lane, nc = min(max(a.cols - c0, 0), 4);
+
+    // ---- 32 rows x 4 columns per lane
+    F raw[MQ_ROWS];
+    const size_t first = (matrix * (size_t)a.rows + (size_t)rw) * (size_t)a.cols + (size_t)c0;      // linear index of the lane's first value
+    const T *src = static_cast<const T *>(a.X) + first;
+    if (vw > 0 && nc == 4) {
+#pragma unroll
+        for (int r = 0; r < MQ_ROWS; r++)
+            __builtin_memcpy(&raw[r], __builtin_assume_aligned(src + (size_t)min(r, vw - 1) * (size_t)a.cols, sizeof(T)), sizeof(F));
+    } else {
+#pragma unroll
+        for (int r = 0; r < MQ_ROWS; r++) {
+            T v[4] = {};
+            if (r < vw)
+                for (int j = 0; j < nc; j++) v[j] = src[(size_t)r * (size_t)a.cols + j];
+            __builtin_memcpy(&raw[r], v, sizeof(F));
+        }
+    }
+    if (vw < MQ_ROWS) {
+#pragma unroll
+        for (int r = 0; r < MQ_ROWS; r++)
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(F) / 4); k++) raw[r][k] = r < vw ? raw[r][k] : 0;
+    }
+
+    // ---- scales along the columns: a block is a lane's own
+    BlockScale cs[4];
+    if (COLS) {
+        unsigned m[4] = {};
+        if constexpr (TYPE == HQ_FP32) {
+#pragma unroll
+            for (int r = 0; r < MQ_ROWS; r++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) m[j] = max(m[j], (unsigned)raw[r][j] & 0x7fffffffu);
+        } else {
+            int p[2] = {};
+#pragma unroll
+            for (int r = 0; r < MQ_ROWS; r++)
+#pragma unroll
+                for (int k = 0; k < 2; k++) p[k] = pk_max_u16(p[k], raw[r][k] & 0x7fff7fff);
+#pragma unroll
+            for (int j = 0; j < 4; j++) m[j] = ((unsigned)p[j >> 1] >> (16 * (j & 1))) & 0xffffu;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            cs[j] = block_scale<SR>(magnitude_bits<TYPE>(m[j]));
+            col_scales[(4 * lane + j) * MX_SCALES + wave] = (uint8_t)cs[j].byte;
+        }
+    }
+
+    // ---- codes, two rows at a time
+    unsigned cc[4][4] = {};                        // codes along the columns: 32 rows of 4 columns
+    uint8_t *out = nullptr;
+    if (ROWS) {
+        // an even lane stores the codes of the even row for itself and its neighbour, an odd lane those of the odd row
+        const size_t row = (matrix * (size_t)a.kc + (size_t)c) * (size_t)a.rows + (size_t)rw;
+        out = a.Q + (row + (lane & 1)) * MX_CODES + (lane >> 1) * 4;
+    }
+    const unsigned pick = lane & 1 ? 0x03020706u : 0x05040100u;           // bytes of (neighbour's: 4 .. 7, own: 0 .. 3)
+#pragma unroll
+    for (int r = 0; r < MQ_ROWS; r += 2) {
+        unsigned both = 0;
+        float x[2][4], u[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[i][j] = four_value<TYPE>(raw[r + i], j);
+            if (SR) {
+                const size_t idx = first + (size_t)(r + i) * (size_t)a.cols;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const unsigned bits = hq_sr_bits((unsigned)(idx + j), (unsigned)((idx + j) >> 32) * 0x85ebca77u + a.sr.k1, a.sr.k0);
+                    u[i][j] = __fmul_rn((float)(bits >> 8), 1.0f / 16777216.0f);
+                }
+            }
+            if (ROWS) {
+                unsigned m;
+                if constexpr (TYPE == HQ_FP32) {
+                    m = max(max((unsigned)raw[r + i][0] & 0x7fffffffu, (unsigned)raw[r + i][1] & 0x7fffffffu),
+                            max((unsigned)raw[r + i][2] & 0x7fffffffu, (unsigned)raw[r + i][3] & 0x7fffffffu));
+                } else {
+                    const unsigned p = (unsigned)pk_max_u16(raw[r + i][0] & 0x7fff7fff, raw[r + i][1] & 0x7fff7fff);
+                    m = max(p & 0xffffu, p >> 16);
+                }
+                m = (unsigned)hq_row_reduce<8>((int)m, HqMax());
+                const BlockScale rs = block_scale<SR>(magnitude_bits<TYPE>(m));
+                unsigned code = 0;
+                if (SR) {
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j++) v[j] = stochastic_value(x[i][j], rs.unit, u[i][j]);
+                    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], 1.0f, 0);
+                    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], 1.0f, 1);
+                } else {
+                    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[i][0], x[i][1], rs.unit, 0);
+                    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[i][2], x[i][3], rs.unit, 1);
+                }
+                both |= ((code & (unsigned)rs.mask) & 0xffffu) << (16 * i);
+                if ((lane & 7) == 0) row_scales[(wave * MQ_ROWS + r + i) * MX_SCALES + (lane >> 3)] = (uint8_t)rs.byte;
+            }
+        }
+        if (ROWS) {
+            const unsigned other = (unsigned)hq_lane_partner<1>((int)both);
+            const unsigned w = __builtin_amdgcn_perm(other, both, pick);
+            if (r + (lane & 1) < vw) *reinterpret_cast<unsigned *>(out + r * MX_CODES) = w;
+        }
+        if (COLS) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float v0 = SR ? stochastic_value(x[0][j], cs[j].unit, u[0][j]) : x[0][j];
+                const float v1 = SR ? stochastic_value(x[1][j], cs[j].unit, u[1][j]) : x[1][j];
+                const float unit = SR ? 1.0f : cs[j].unit;
+                unsigned &d = cc[j][r / 8];
+                switch (r % 8 / 2) {               // (the byte is part of the instruction)
+                case 0: d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v0, v1, unit, 0); break;
+                case 1: d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v0, v1, unit, 1); break;
+                case 2: d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v0, v1, unit, 2); break;
+                default: d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v0, v1, unit, 3); break;
+                }
+            }
+        }
+    }
+    if (COLS) {
+        // column 4 * lane + j is row j * 64 + lane of the LDS tile
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            *reinterpret_cast<v4i *>(codes + (j * 64 + lane) * MQ_PITCH + 16 * wave) =
+                v4i{(int)cc[j][0] & cs[j].mask, (int)cc[j][1] & cs[j].mask, (int)cc[j][2] & cs[j].mask, (int)cc[j][3] & cs[j].mask};
+    }
+    __syncthreads();
+    if (ROWS) {
+        // 32 rows x 8 bytes of a wavefront: one run
+        const size_t row = (matrix * (size_t)a.kc + (size_t)c) * (size_t)a.rows + (size_t)rw;
+        if ((lane >> 1) < vw)
+            *reinterpret_cast<unsigned *>(a.S + row * MX_SCALES + 4 * lane) = *reinterpret_cast<const unsigned *>(row_scales + wave * MQ_ROWS * MX_SCALES + 4 * lane);
+    }
+    if (COLS) {
+        const int ncols = min(a.cols - c * MX_CHUNK, MX_CHUNK);
+        const size_t col = (size_t)y * (size_t)a.cols + (size_t)c * MX_CHUNK;
+        for (int k = threadIdx.x; k < ncols * (MX_CODES / 16); k += 64 * NW) {
+            const int n = k >> 3, part = k & 7;
+            *reinterpret_cast<v4i *>(a.Qt + (col + n) * MX_CODES + 16 * part) =
+                *reinterpret_cast<const v4i *>(codes + ((n & 3) * 64 + (n >> 2)) * MQ_PITCH + 16 * part);
+        }
+        for (int k = threadIdx.x; k < ncols * (MX_SCALES / 4); k += 64 * NW)
+            *reinterpret_cast<unsigned *>(a.St + col * MX_SCALES + 4 * k) = *reinterpret_cast<const unsigned *>(col_scales + 4 * k);
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+struct DequantizeArgs {
+    const uint8_t *Q, *S;
+    const int *offs;
+    void *X;
+    int rows, n, segments;
+    int chunks;                                    // of a matrix (without offs)
+    int tiles;                                     // row tiles
+};
+
+constexpr int MD_ROWS = 32;                        // rows of a workgroup: 8 at a time, 32 lanes a row, 8 values a lane
+
+template <int TYPE> __global__ __launch_bounds__(HQ_THREADS) void mx4_dequantize_kernel(const DequantizeArgs a)
+{
+    typedef typename HqReal<TYPE>::T T;
+    const unsigned y = blockIdx.x / (unsigned)a.tiles;
+    const int tile = (int)(blockIdx.x - y * (unsigned)a.tiles);
+    int k0, valid;                                 // the chunk's place on the axis, its values
+    size_t matrix = 0;
+    if (a.offs) {
+        const HqSegment s = hq_segment_of<MX_CHUNK>(a.offs, a.segments, a.n, (int)y);
+        if (s.e < 0) return;
+        k0 = s.first + s.unit * MX_CHUNK;
+        valid = min(MX_CHUNK, s.end - k0);
+    } else {
+        matrix = y / (unsigned)a.chunks;
+        k0 = (int)(y - (unsigned)matrix * (unsigned)a.chunks) * MX_CHUNK;
+        valid = min(MX_CHUNK, a.n - k0);
+    }
+    const int part = threadIdx.x & 31, have = min(max(valid - 8 * part, 0), 8);
+    for (int r = tile * MD_ROWS + (threadIdx.x >> 5); r < min(a.rows, (tile + 1) * MD_ROWS); r += HQ_THREADS / 32) {
+        const size_t row = (size_t)y * (size_t)a.rows + (size_t)r;
+        const unsigned code = *reinterpret_cast<const unsigned *>(a.Q + row * MX_CODES + 4 * part);
+        const unsigned byte = a.S[row * MX_SCALES + (part >> 2)];
+        const float scale = __uint_as_float(byte == 255 ? 0x7fc00000u : byte ? byte << 23 : 0x400000u);
+        T v[8];
+        auto two = [&](v2f p, int k) __attribute__((always_inline)) {
+            v[k] = HqReal<TYPE>::store(__fmul_rn(p[0], scale)); v[k + 1] = HqReal<TYPE>::store(__fmul_rn(p[1], scale));
+        };
+        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 0), 0);
+        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 1), 2);
+        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 2), 4);
+        two(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, 1.0f, 3), 6);
+        T *dst = static_cast<T *>(a.X) + (matrix * (size_t)a.rows + (size_t)r) * (size_t)a.n + (size_t)(k0 + 8 * part);
+        if (have == 8) __builtin_memcpy(__builtin_assume_aligned(dst, sizeof(T)), v, sizeof(v));
+        else
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (j < have) dst[j] = v[j];
+    }
+}
+
+inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+inline int launch_status() { return hipGetLastError() == hipSuccess ? HQ_OK : HQ_E_HIP; }
+
+template <int TYPE, bool SR> int launch_quantize(const QuantizeArgs &a, unsigned blocks, hipStream_t s)
+{
+    constexpr int CHUNK_WAVES = MX_CHUNK / MQ_ROWS;
+    if (a.Qt && a.Q)
+        hipLaunchKernelGGL((mx4_quantize_kernel<TYPE, true, true, SR, CHUNK_WAVES>), dim3(blocks), dim3(64 * CHUNK_WAVES), 0, s, a);
+    else if (a.Qt)
+        hipLaunchKernelGGL((mx4_quantize_kernel<TYPE, false, true, SR, CHUNK_WAVES>), dim3(blocks), dim3(64 * CHUNK_WAVES), 0, s, a);
+    else
+        hipLaunchKernelGGL((mx4_quantize_kernel<TYPE, true, false, SR, 1>), dim3(blocks), dim3(64), 0, s, a);
+    return launch_status();
+}
+
+int quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs, const uint64_t *seed,
+             uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream)
+{
+    if (!hq_mx4_type_ok(xtype) || (!Q != !S) || (!Qt != !St) || (!Q && !Qt)) return HQ_E_BADARG;
+    if (rows < 0 || cols < 1 || batch < 1 || rows >= MX_MOST || cols >= MX_MOST || (offs && batch > HQ_MX4_MAX_SEGMENTS)) return HQ_E_BADSHAPE;
+    if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(S, 16) || misaligned(Qt, 16) || misaligned(St, 16) || misaligned(offs, 4)) return HQ_E_BADARG;
+    QuantizeArgs a = {};
+    a.X = X; a.offs = offs; a.Q = Q; a.S = S; a.Qt = Qt; a.St = St;
+    a.rows = rows; a.cols = cols; a.segments = batch;
+    a.kc = (int)hq_mx4_chunks(cols, 1);
+    // row tiles: whole chunks if there are codes along the columns, otherwise a wavefront's rows
+    const int tile = Qt ? MX_CHUNK : MQ_ROWS;
+    a.tiles = (rows + tile - 1) / tile;
+    const long y = offs ? (rows - std::min(batch, rows)) / tile + std::min(batch, rows) : (long)a.tiles * batch;
+    if ((double)y * a.kc >= 2147483648.0) return HQ_E_BADSHAPE;
+    if (y == 0) return HQ_OK;
+    if (!X) return HQ_E_BADARG;
+    if (seed) a.sr = HqSr{(unsigned)*seed, (unsigned)(*seed >> 32)};
+    const unsigned blocks = (unsigned)(y * a.kc);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    switch (xtype) {
+    case HQ_FP32: return seed ? launch_quantize<HQ_FP32, true>(a, blocks, s) : launch_quantize<HQ_FP32, false>(a, blocks, s);
+    case HQ_BF16: return seed ? launch_quantize<HQ_BF16, true>(a, blocks, s) : launch_quantize<HQ_BF16, false>(a, blocks, s);
+    default:      return seed ? launch_quantize<HQ_FP16, true>(a, blocks, s) : launch_quantize<HQ_FP16, false>(a, blocks, s);
+    }
+}
+
+} // namespace
+
+extern "C" {
+
+int64_t hq_mx4_chunks(int64_t n, int32_t segments)
+{
+    if (n < 0 || n >= MX_MOST || segments < 1 || segments > HQ_MX4_MAX_SEGMENTS) return 0;
+    // a first value opens a chunk for every segment that has one; of the rest, every 256 more open another
+    const int64_t used = std::min<int64_t>(segments, n);
+    return (n - used) / MX_CHUNK + used;
+}
+
+int hq_mx4_quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
+                    uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream)
+{
+    return quantize(xtype, X, rows, cols, batch, offs, nullptr, Q, S, Qt, St, stream);
+}
+
+int hq_mx4_quantize_sr(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
+                       uint64_t seed, uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream)
+{
+    return quantize(xtype, X, rows, cols, batch, offs, &seed, Q, S, Qt, St, stream);
+}
+
+int hq_mx4_dequantize(const uint8_t *Q, const uint8_t *S, int32_t rows, int32_t n, int32_t batch, const int32_t *offs,
+                      int32_t xtype, void *X, void *stream)
+{
+    if (!hq_mx4_type_ok(xtype)) return HQ_E_BADARG;
+    if (rows < 0 || n < 0 || batch < 1 || rows >= MX_MOST || n >= MX_MOST || (offs && batch > HQ_MX4_MAX_SEGMENTS)) return HQ_E_BADSHAPE;
+    if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(S, 16) || misaligned(offs, 4)) return HQ_E_BADARG;
+    DequantizeArgs a = {};
+    a.Q = Q; a.S = S; a.offs = offs; a.X = X; a.rows = rows; a.n = n; a.segments = batch;
+    a.chunks = (int)hq_mx4_chunks(n, 1);
+    a.tiles = (rows + MD_ROWS - 1) / MD_ROWS;
+    const long y = offs ? (long)hq_mx4_chunks(n, batch) : (long)a.chunks * batch;
+    if ((double)y * a.tiles >= 2147483648.0) return HQ_E_BADSHAPE;
+    if (y == 0 || a.tiles == 0) return HQ_OK;
+    if (!Q || !S || !X) return HQ_E_BADARG;
+    const dim3 grid((unsigned)(y * a.tiles)), threads(HQ_THREADS);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    switch (xtype) {
+    case HQ_FP32: hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_FP32>, grid, threads, 0, s, a); break;
+    case HQ_BF16: hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_BF16>, grid, threads, 0, s, a); break;
+    default:      hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_FP16>, grid, threads, 0, s, a); break;
+    }
+    return launch_status();
+}
+
+} // extern "C"
