@@ -3,7 +3,7 @@
 //
 //   out[m][n] = sum_blocks 2^(sa[m][b] + sb[n][b] - 254) sum_{k in b} a[m][k] b[n][k]
 //
-// on the scaled MFMA (32 x 32 x 64, fp4 x fp4): a lane holds one block of a row, 16 bytes, and its scale byte; the products are summed
+// on the scaled MFMA (16 x 16 x 128, fp4 x fp4): a lane holds one block of a row, 16 bytes, and its scale byte; the products are summed
 // in fp32 by the matrix pipe.  Containers are cut along the contraction into chunks of 256 values, 128 bytes a row; the rows of a chunk
 // follow each other, so a tile's operands of one chunk are one run of memory, at any row offset, and there is no tail along the contraction
 // (behind its end the codes are 0).
@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <cstdlib>
 
 namespace {
 
@@ -31,11 +32,6 @@ struct ProductArgs {
     int out_type;
 };
 
-template <int SCALE_BYTE> __device__ inline v16f mfma32(v4i a, v4i b, v16f c, int sa, int sb)
-{
-    const v8i a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a8, b8, c, 4, 4, SCALE_BYTE, sa, SCALE_BYTE, sb);
-}
 template <int SCALE_BYTE> __device__ inline v4f mfma16(v4i a, v4i b, v4f c, int sa, int sb)
 {
     const v8i a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1), b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
@@ -65,18 +61,18 @@ template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const
 
 // ---------------------------------------------------------------------------------------
 // Tiles of BM x BN outputs, WM x WN wavefronts of (BM / WM) x (BN / WN) each.  A stage is one chunk of the tile's rows of A and B, straight
-// from memory into one of two LDS buffers; the 16-byte blocks of a row are XOR-swizzled by the row.
+// from memory into one of two LDS buffers; the 16-byte blocks of a row are XOR-swizzled by the row.  A step is half a chunk: a lane's two blocks.
 // ---------------------------------------------------------------------------------------
 template <int BM, int BN, int WM, int WN, int GROUP>
 __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArgs a)
 {
-    constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
+    constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int CODE_LOADS = (BM + BN) / 8 / NW, SCALE_LOADS = (BM + BN) / 32 / NW;
-    static_assert(CODE_LOADS * 8 * NW == BM + BN && SCALE_LOADS * 32 * NW == BM + BN, "whole loads");
+    static_assert(BM % (32 * NW) == 0 && BN % (32 * NW) == 0, "a load of all wavefronts belongs to one operand");
     constexpr int STAGE = (BM + BN) * (MX_CODES + MX_SCALES);
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int half = lane >> 5, r32 = lane & 31, wm = wave / WN, wn = wave % WN;
+    const int group = lane >> 4, r16 = lane & 15, wm = wave / WN, wn = wave % WN;
 
     // ---- which tile: each XCD takes a run of them, in bands of 8 row tiles
     const int per_split = a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? a.experts : 1);
@@ -85,7 +81,21 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
     const int per = per_split / 8;
     if (tile < per * 8) tile = (tile & 7) * per + (tile >> 3);
     int e = 0;
-    if (GROUP == BY_CHUNKS) { e = tile / (a.m_tiles * a.n_tiles); tile -= e * (a.m_tiles * a.n_tiles); }
+    if (GROUP == BY_CHUNKS) {
+        // (every expert's tiles over all XCDs: their contractions differ in length)
+        const int mn = a.m_tiles * a.n_tiles, share = mn / 8, b = blockIdx.x - split * per_split;
+        if (share) {
+            if (b < share * 8 * a.experts) {
+                const int x = b & 7, t = b >> 3;
+                e = t / share;
+                tile = x * share + t - e * share;
+            } else {
+                const int t = b - share * 8 * a.experts, left = mn - 8 * share;
+                e = t / left;
+                tile = 8 * share + t - e * left;
+            }
+        } else { e = b / mn; tile = b - e * mn; }
+    }
     const int band = tile / (8 * a.n_tiles), in_band = min(8, a.m_tiles - 8 * band), rest = tile - band * 8 * a.n_tiles;
     const int tile_n = rest / in_band, tile_m = 8 * band + rest - tile_n * in_band;
 
@@ -111,121 +121,136 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
     if (GROUP != BY_ROWS) b_chunk0 = (size_t)chunk0;
 
     // ---- loads: 8 rows of codes or 32 rows of scales each; rows past the end repeat the last (never stored)
-    const uint8_t *code_base[CODE_LOADS], *scale_base[SCALE_LOADS];
+    const uint8_t *code_a = a.A + ((size_t)chunk0 * (size_t)a.M + (size_t)m0) * MX_CODES, *scale_a = a.As + ((size_t)chunk0 * (size_t)a.M + (size_t)m0) * MX_SCALES;
+    const uint8_t *code_b = a.B + (b_chunk0 * (size_t)a.N + (size_t)n0) * MX_CODES, *scale_b = a.Bs + (b_chunk0 * (size_t)a.N + (size_t)n0) * MX_SCALES;
     unsigned code_off[CODE_LOADS], scale_off[SCALE_LOADS];
-    const size_t a_row0 = (size_t)chunk0 * (size_t)a.M + (size_t)m0, b_row0 = b_chunk0 * (size_t)a.N + (size_t)n0;
+    // Of a wavefront's columns, LDS row 16 * j + r holds this one, so that a lane has neighbours of 16 bytes and 16 lanes a run of 256.
+    const bool wide = TN == 8 && a.splits == 1 && a.out_type != HQ_FP32;
+    auto column_of = [&](int j, int r) __attribute__((always_inline)) { return wide ? 8 * r + j : (j & ~3) * 16 + 4 * r + (j & 3); };
     auto row_of = [&](int row) __attribute__((always_inline)) {          // LDS row -> row of its operand, from the tile's first
-        const bool is_a = row < BM;
-        const int r = is_a ? row : ((row - BM) & ~31) + hq_sigma32((row - BM) & 31);
-        return min(r, is_a ? m_end - 1 - m0 : a.N - 1 - n0);
+        if (row < BM) return min(row, m_end - 1 - m0);
+        const int c = row - BM, in = c % (16 * TN);
+        return min(c - in + column_of(in >> 4, in & 15), a.N - 1 - n0);
     };
 #pragma unroll
     for (int k = 0; k < CODE_LOADS; k++) {
-        const int first = 8 * (NW * k + wave), row = first + (lane >> 3);
-        code_base[k] = first < BM ? a.A + a_row0 * MX_CODES : a.B + b_row0 * MX_CODES;
+        const int row = 8 * (NW * k + wave) + (lane >> 3);
         code_off[k] = (unsigned)row_of(row) * MX_CODES + 16u * (unsigned)((lane & 7) ^ ((row >> 1) & 7));
     }
 #pragma unroll
-    for (int k = 0; k < SCALE_LOADS; k++) {
-        const int first = 32 * (NW * k + wave), row = first + (lane >> 1);
-        scale_base[k] = first < BM ? a.As + a_row0 * MX_SCALES : a.Bs + b_row0 * MX_SCALES;
-        scale_off[k] = (unsigned)row_of(row) * MX_SCALES + 4u * (unsigned)(lane & 1);
-    }
-    const unsigned lds0 = hq_lds_address(smem);
-    auto request = [&](int buf) __attribute__((always_inline)) {         // the next stage
-        const unsigned dst = lds0 + buf * STAGE;
-#pragma unroll
-        for (int k = 0; k < CODE_LOADS; k++) {
-            hq_lds_load16(reinterpret_cast<const int8_t *>(code_base[k]), code_off[k], dst + 1024 * (NW * k + wave));
-            code_base[k] += (size_t)(8 * (NW * k + wave) < BM ? a.M : a.N) * MX_CODES;
-        }
-#pragma unroll
-        for (int k = 0; k < SCALE_LOADS; k++) {
-            hq_lds_load4(scale_base[k], scale_off[k], dst + (BM + BN) * MX_CODES + 256 * (NW * k + wave));
-            scale_base[k] += (size_t)(32 * (NW * k + wave) < BM ? a.M : a.N) * MX_SCALES;
+    for (int k = 0; k < SCALE_LOADS; k++) scale_off[k] = (unsigned)row_of(32 * (NW * k + wave) + (lane >> 1)) * MX_SCALES + 4u * (unsigned)(lane & 1);
+    const unsigned lds0 = hq_lds_address(smem) + 1024 * wave, lds1 = hq_lds_address(smem) + (BM + BN) * MX_CODES + 256 * wave;
+    auto request = [&](int buf, int k) __attribute__((always_inline)) {  // load k of the next stage
+        if (k < CODE_LOADS)
+            hq_lds_load16(reinterpret_cast<const int8_t *>(8 * NW * k < BM ? code_a : code_b), code_off[k], lds0 + buf * STAGE + 1024 * NW * k);
+        else {
+            const int q = k - CODE_LOADS;
+            hq_lds_load4(32 * NW * q < BM ? scale_a : scale_b, scale_off[q], lds1 + buf * STAGE + 256 * NW * q);
         }
     };
+    constexpr int LOADS = CODE_LOADS + SCALE_LOADS;
+    auto requested = [&]() __attribute__((always_inline)) {
+        code_a += (size_t)a.M * MX_CODES; scale_a += (size_t)a.M * MX_SCALES;
+        code_b += (size_t)a.N * MX_CODES; scale_b += (size_t)a.N * MX_SCALES;
+    };
 
-    v16f acc[TM][TN];
+    v4f acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; i++)
 #pragma unroll
-        for (int j = 0; j < TN; j++)
-#pragma unroll
-            for (int k = 0; k < 16; k++) acc[i][j][k] = 0.0f;
+        for (int j = 0; j < TN; j++) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
-    v4i fa[2][TM], fb[2][TN];
-    int sa[TM], sb[TN];
-    const int row_a = wm * (BM / WM) + r32, row_b = BM + wn * (BN / WN) + r32;
-    auto scales = [&](int buf) __attribute__((always_inline)) {
-        const uint8_t *p = smem + buf * STAGE + (BM + BN) * MX_CODES + 4 * half;
-#pragma unroll
-        for (int i = 0; i < TM; i++) sa[i] = *reinterpret_cast<const int *>(p + (row_a + 32 * i) * MX_SCALES);
-#pragma unroll
-        for (int j = 0; j < TN; j++) sb[j] = *reinterpret_cast<const int *>(p + (row_b + 32 * j) * MX_SCALES);
-    };
-    auto fragments = [&](int buf, int step) __attribute__((always_inline)) {
-        const uint8_t *p = smem + buf * STAGE + 16 * ((4 * half + step) ^ ((r32 >> 1) & 7));
-#pragma unroll
-        for (int i = 0; i < TM; i++) fa[step & 1][i] = *reinterpret_cast<const v4i *>(p + (row_a + 32 * i) * MX_CODES);
-#pragma unroll
-        for (int j = 0; j < TN; j++) fb[step & 1][j] = *reinterpret_cast<const v4i *>(p + (row_b + 32 * j) * MX_CODES);
-    };
-
-    if (nst > 0) request(0);
-    if (nst > 1) { request(1); asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CODE_LOADS + SCALE_LOADS) : "memory"); }
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (nst > 0) { scales(0); fragments(0, 0); }
+    // Fragments of A are kept twice, those of B once: a step goes through them in turn and each is loaded for the next step when it has been used.
+    v4i fa[2][TM], fb[TN];
+    int sa[TM], sa_next[TM], sb[TN];
+    const int row_a = wm * (BM / WM) + r16, row_b = BM + wn * (BN / WN) + r16;
     int cur = 0;
-    for (int s = 0; s < nst; s++) {
-        auto multiply = [&](auto step, const int *qa, const int *qb) __attribute__((always_inline)) {
-            constexpr int K = decltype(step)::value;
+    auto codes_at = [&](int row, int step) __attribute__((always_inline)) {
+        return *reinterpret_cast<const v4i *>(smem + cur * STAGE + 16 * ((2 * group + step) ^ ((r16 >> 1) & 7)) + row * MX_CODES);
+    };
+    auto scale_at = [&](int row) __attribute__((always_inline)) {
+        return (int)*reinterpret_cast<const unsigned short *>(smem + cur * STAGE + (BM + BN) * MX_CODES + 2 * group + row * MX_SCALES);
+    };
+    if (nst > 0) {
 #pragma unroll
-            for (int i = 0; i < TM; i++)
+        for (int k = 0; k < LOADS; k++) request(0, k);
+        requested();
+        if (nst > 1) {
 #pragma unroll
-                for (int j = 0; j < TN; j++) acc[i][j] = mfma32<K>(fb[K & 1][j], fa[K & 1][i], acc[i][j], qb[j], qa[i]);
-        };
-        fragments(cur, 1);
-        multiply(std::integral_constant<int, 0>(), sa, sb);
-        fragments(cur, 2);
-        multiply(std::integral_constant<int, 1>(), sa, sb);
-        fragments(cur, 3);
-        multiply(std::integral_constant<int, 2>(), sa, sb);
-        int qa[TM], qb[TN];
+            for (int k = 0; k < LOADS; k++) request(1, k);
+            requested();
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < TM; i++) qa[i] = sa[i];
+        for (int i = 0; i < TM; i++) { fa[0][i] = codes_at(row_a + 16 * i, 0); sa[i] = scale_at(row_a + 16 * i); }
 #pragma unroll
-        for (int j = 0; j < TN; j++) qb[j] = sb[j];
-        if (s + 1 < nst) {
+        for (int j = 0; j < TN; j++) { fb[j] = codes_at(row_b + 16 * j, 0); sb[j] = scale_at(row_b + 16 * j); }
+    }
+    // `next`: there is a stage after this one; `more`: and another one.  (Nothing moves across the lines; no branches, which the compiler would
+    // let products sink below.)
+    auto stage = [&](auto more, auto next) __attribute__((always_inline)) {
+        constexpr bool MORE = decltype(more)::value, NEXT = decltype(next)::value;
+#pragma unroll
+        for (int j = 0; j < TN; j++) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < TM; i++) acc[i][j] = mfma16<0>(fa[0][i], fb[j], acc[i][j], sa[i], sb[j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (j < TM) fa[1][j] = codes_at(row_a + 16 * j, 1);
+            fb[j] = codes_at(row_b + 16 * j, 1);
+        }
+        const int freed = cur;
+        if (NEXT) {
             // all fragments of this stage are in registers at the barrier: its buffer takes the stage after next
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            if (s + 2 < nst) request(cur);
             cur ^= 1;
-            scales(cur);
-            fragments(cur, 0);
         }
-        multiply(std::integral_constant<int, 3>(), qa, qb);
-    }
-
-    // ---- 16 consecutive columns of a row per lane and 32 x 32 block
-    auto finish = [&](auto type, void *out) __attribute__((always_inline)) {
-        constexpr int TYPE = decltype(type)::value;
-        typedef typename HqReal<TYPE>::T T;
 #pragma unroll
-        for (int i = 0; i < TM; i++) {
-            const int m = m0 + wm * (BM / WM) + 32 * i + r32;
-            if (m >= m_end) continue;
+        for (int j = 0; j < TN; j++) {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < TN; j++) {
-                const int n = n0 + wn * (BN / WN) + 32 * j + 16 * half;
-                float v[16];
+            for (int i = 0; i < TM; i++) acc[i][j] = mfma16<1>(fa[1][i], fb[j], acc[i][j], sa[i], sb[j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (MORE) {
 #pragma unroll
-                for (int k = 0; k < 16; k++) v[k] = acc[i][j][k];
-                store_run<TYPE, 16>(static_cast<T *>(out) + ((size_t)m * (size_t)a.N + (size_t)n), v, n, a.N);
+                for (int k = j * LOADS / TN; k < (j + 1) * LOADS / TN; k++) request(freed, k);
+            }
+            if (NEXT) {
+                if (j < TM) { fa[0][j] = codes_at(row_a + 16 * j, 0); sa_next[j] = scale_at(row_a + 16 * j); }
+                fb[j] = codes_at(row_b + 16 * j, 0);
+                sb[j] = scale_at(row_b + 16 * j);
             }
         }
+        if (MORE) requested();
+        if (NEXT) {
+#pragma unroll
+            for (int i = 0; i < TM; i++) sa[i] = sa_next[i];
+        }
+    };
+    int s = 0;
+    for (; s + 2 < nst; s++) stage(std::true_type(), std::true_type());
+    if (s + 1 < nst) { stage(std::false_type(), std::true_type()); s++; }
+    if (s < nst) stage(std::false_type(), std::false_type());
+
+    // ---- a lane's columns of a row, 16 bytes at a time
+    auto finish = [&](auto type, void *out) __attribute__((always_inline)) {
+        constexpr int TYPE = decltype(type)::value, RUN = TYPE == HQ_FP32 ? 4 : TN;
+        typedef typename HqReal<TYPE>::T T;
+        const int m = m0 + wm * (BM / WM) + 4 * group, n = n0 + wn * (BN / WN) + RUN * r16;
+        T *dst = static_cast<T *>(out) + ((size_t)m * (size_t)a.N + (size_t)n);
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+                for (int j = 0; j < TN; j += RUN) {
+                    float v[RUN];
+#pragma unroll
+                    for (int c = 0; c < RUN; c++) v[c] = acc[i][j + c][k];
+                    if (m + 16 * i + k < m_end) store_run<TYPE, RUN>(dst + (size_t)(16 * i + k) * (size_t)a.N + 16 * j, v, n + 16 * j, a.N);
+                }
     };
     const size_t expert_out = GROUP == BY_CHUNKS ? (size_t)e * (size_t)a.M * (size_t)a.N : 0;
     if (a.splits > 1) finish(std::integral_constant<int, HQ_FP32>(), a.part + (size_t)split * a.outputs + expert_out);
@@ -346,7 +371,8 @@ Plan plan_of(const hq_mx4_problem *p, int group)
         const long chunks = hq_mx4_chunks(p->K, 1) / p->experts;
         while (tiles * splits < 512 && chunks / (splits * 2) >= 4) splits *= 2;
     }
-    return Plan{128, splits};
+    const long large = (long)tiles_of(p->M, 256) * tiles_of(p->N, 256) * (group == BY_CHUNKS ? p->experts : 1);
+    return Plan{splits == 1 && large >= 256 && !getenv("MX_SMALL") ? 256 : 128, splits};
 }
 
 size_t outputs_of(const hq_mx4_problem *p, int group)
@@ -401,7 +427,7 @@ template <int GROUP> int product(const hq_mx4_problem *p, const uint8_t *A, cons
     a.n_tiles = tiles_of(p->N, side);
     const double blocks = (double)a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? p->experts : 1) * a.splits;
     if (blocks >= 2147483648.0) return HQ_E_BADSHAPE;
-    rc = launch_tile<128, 128, 2, 2, GROUP>(a, (long)blocks, s);
+    rc = side == 256 ? launch_tile<256, 256, 4, 2, GROUP>(a, (long)blocks, s) : launch_tile<128, 128, 2, 2, GROUP>(a, (long)blocks, s);
     if (rc != HQ_OK || a.splits == 1) return rc;
     const unsigned join = (unsigned)std::min<size_t>((a.outputs / 4 + HQ_THREADS) / HQ_THREADS, 2048);
     switch (p->out_type) {
