@@ -12,7 +12,6 @@
 
 #include <algorithm>
 #include <type_traits>
-#include <cstdlib>
 
 namespace {
 
@@ -21,8 +20,7 @@ enum { DENSE = 0, BY_ROWS = 1, BY_CHUNKS = 2 };   // one product; rows of A by e
 struct ProductArgs {
     const uint8_t *A, *As, *B, *Bs;
     const int *offs;
-    void *out;
-    float *part;                   // partial sums of split contractions [splits][outputs], or NULL
+    void *out;                     // split contractions: their partial sums [splits][outputs], fp32
     size_t outputs;
     int M, N;                      // rows of A and of out (BY_ROWS: of all experts together), rows of B
     int chunks;                    // of the contraction (BY_CHUNKS: the most that the segments can have)
@@ -42,6 +40,8 @@ template <int SCALE_BYTE> __device__ inline v4f mfma16(v4i a, v4i b, v4f c, int 
 // wait states that the matrix pipe needs before its registers are read (it puts them before the second store).
 __device__ inline void mfma16_done(v4f &c) { asm volatile("s_nop 15" : "+v"(c)); }
 
+typedef int HqUnaligned16 __attribute__((ext_vector_type(4), aligned(2)));
+
 // COUNT consecutive outputs from column n on, of N, to `dst` (the address of column n); rounded once.
 template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const float *v, int n, int N)
 {
@@ -51,7 +51,13 @@ template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const
         T t[COUNT];
 #pragma unroll
         for (int e = 0; e < COUNT; e++) t[e] = HqReal<TYPE>::store(v[e]);
-        __builtin_memcpy(__builtin_assume_aligned(d, sizeof(T)), t, sizeof(t));
+        if constexpr (sizeof(t) == 16) {
+            // (past L2, which the operands of the tiles to come are to stay in: weight gradients of 16 experts, 4096 x 1024 fp32 over 16384 rows,
+            // 104 -> 81 us; forward pass of 8 experts, 8192 x 4096 bf16, 42 -> 39)
+            v4i x;
+            __builtin_memcpy(&x, t, 16);
+            __builtin_nontemporal_store((HqUnaligned16)x, reinterpret_cast<HqUnaligned16 *>(d));
+        } else __builtin_memcpy(__builtin_assume_aligned(d, sizeof(T)), t, sizeof(t));
     } else {
 #pragma unroll
         for (int e = 0; e < COUNT; e++)
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
     const uint8_t *code_b = a.B + (b_chunk0 * (size_t)a.N + (size_t)n0) * MX_CODES, *scale_b = a.Bs + (b_chunk0 * (size_t)a.N + (size_t)n0) * MX_SCALES;
     unsigned code_off[CODE_LOADS], scale_off[SCALE_LOADS];
     // Of a wavefront's columns, LDS row 16 * j + r holds this one, so that a lane has neighbours of 16 bytes and 16 lanes a run of 256.
-    const bool wide = TN == 8 && a.splits == 1 && a.out_type != HQ_FP32;
+    const bool wide = TN == 8 && a.out_type != HQ_FP32;
     auto column_of = [&](int j, int r) __attribute__((always_inline)) { return wide ? 8 * r + j : (j & ~3) * 16 + 4 * r + (j & 3); };
     auto row_of = [&](int row) __attribute__((always_inline)) {          // LDS row -> row of its operand, from the tile's first
         if (row < BM) return min(row, m_end - 1 - m0);
@@ -252,11 +258,10 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
                     if (m + 16 * i + k < m_end) store_run<TYPE, RUN>(dst + (size_t)(16 * i + k) * (size_t)a.N + 16 * j, v, n + 16 * j, a.N);
                 }
     };
-    const size_t expert_out = GROUP == BY_CHUNKS ? (size_t)e * (size_t)a.M * (size_t)a.N : 0;
-    if (a.splits > 1) finish(std::integral_constant<int, HQ_FP32>(), a.part + (size_t)split * a.outputs + expert_out);
-    else if (a.out_type == HQ_FP32) finish(std::integral_constant<int, HQ_FP32>(), static_cast<float *>(a.out) + expert_out);
-    else if (a.out_type == HQ_BF16) finish(std::integral_constant<int, HQ_BF16>(), static_cast<unsigned short *>(a.out) + expert_out);
-    else finish(std::integral_constant<int, HQ_FP16>(), static_cast<unsigned short *>(a.out) + expert_out);
+    const size_t first = (GROUP == BY_CHUNKS ? (size_t)e * (size_t)a.M * (size_t)a.N : 0) + (size_t)split * a.outputs;
+    if (a.out_type == HQ_FP32) finish(std::integral_constant<int, HQ_FP32>(), static_cast<float *>(a.out) + first);
+    else if (a.out_type == HQ_BF16) finish(std::integral_constant<int, HQ_BF16>(), static_cast<unsigned short *>(a.out) + first);
+    else finish(std::integral_constant<int, HQ_FP16>(), static_cast<unsigned short *>(a.out) + first);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -323,25 +328,31 @@ template <int MT, int GROUP> __global__ __launch_bounds__(512) void mx4_row_kern
     }
 }
 
-// ---- partial sums of split contractions, added in order -----------------------------------
-template <int TYPE> __global__ __launch_bounds__(HQ_THREADS) void mx4_join_kernel(const float *part, size_t outputs, int splits, void *out)
+// ---- partial sums of split contractions, added in order: WIDTH outputs a lane -------------
+template <int TYPE, int WIDTH> __global__ __launch_bounds__(HQ_THREADS) void mx4_join_kernel(const float *part, size_t outputs, int splits, void *out)
 {
     typedef typename HqReal<TYPE>::T T;
-    const size_t groups = (outputs + 3) / 4;
-    for (size_t g = (size_t)blockIdx.x * HQ_THREADS + threadIdx.x; g < groups; g += (size_t)gridDim.x * HQ_THREADS) {
-        const int have = (int)min((size_t)4, outputs - 4 * g);
-        float v[4] = {};
-        for (int s = 0; s < splits; s++) {
-            const float *p = part + (size_t)s * outputs + 4 * g;
-            float x[4] = {};
-            if (have == 4) __builtin_memcpy(x, __builtin_assume_aligned(p, 4), 16);
-            else
-                for (int j = 0; j < have; j++) x[j] = p[j];
+    typedef float V __attribute__((ext_vector_type(WIDTH)));
+    for (size_t g = ((size_t)blockIdx.x * HQ_THREADS + threadIdx.x) * WIDTH; g < outputs; g += (size_t)gridDim.x * HQ_THREADS * WIDTH) {
+        V v = *reinterpret_cast<const V *>(part + g);
+#pragma unroll 4
+        for (int s = 1; s < splits; s++) {
+            const V x = *reinterpret_cast<const V *>(part + (size_t)s * outputs + g);
 #pragma unroll
-            for (int j = 0; j < 4; j++) v[j] = __fadd_rn(v[j], x[j]);
+            for (int j = 0; j < WIDTH; j++) v[j] = __fadd_rn(v[j], x[j]);
         }
-        store_run<TYPE, 4>(static_cast<T *>(out) + 4 * g, v, 0, have);
+        T t[WIDTH];
+#pragma unroll
+        for (int j = 0; j < WIDTH; j++) t[j] = HqReal<TYPE>::store(v[j]);
+        __builtin_memcpy(static_cast<T *>(out) + g, t, sizeof(t));
     }
+}
+template <int TYPE> void launch_join(const float *part, size_t outputs, int splits, void *out, hipStream_t s)
+{
+    const int width = outputs % 4 == 0 ? 4 : 1;                          // (16-byte loads of every partial sum)
+    const unsigned blocks = (unsigned)std::min<size_t>((outputs / width + HQ_THREADS - 1) / HQ_THREADS, 8192);
+    if (width == 4) hipLaunchKernelGGL((mx4_join_kernel<TYPE, 4>), dim3(blocks), dim3(HQ_THREADS), 0, s, part, outputs, splits, out);
+    else            hipLaunchKernelGGL((mx4_join_kernel<TYPE, 1>), dim3(blocks), dim3(HQ_THREADS), 0, s, part, outputs, splits, out);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -357,22 +368,43 @@ int check_product(const hq_mx4_problem *p, bool grouped)
     return HQ_OK;
 }
 
-struct Plan { int tile, splits; };                 // tile: 0 few rows; otherwise the tile's side
+struct Plan { int side, splits; };                 // side: 1, 2: few rows, 16 of them at a time or 32; otherwise the tile's side
 
 int tiles_of(long n, int side) { return (int)((n + side - 1) / side); }
 
-// Contractions are split where tiles alone leave compute units idle.
+// Microseconds that a launch takes, so that tile and split can be chosen: a start, the stages of a workgroup, and the bytes of the outputs.  A
+// stage takes its latency while the compute units hold all workgroups at once, from there on their share of the card.  Fitted to (this / measured, us)
+// 1024 x 4096 x 4096 to bf16 in tiles of 64, 128, 256: 18.3 / 16.7, 16.9 / 17.0, 23.4 / 23.2; 4096 x 4096 x 4096 64.3 / 62.0, 53.4 / 48.0,
+// 42.6 / 35.6; 256 x 4096 x 4096 11.3 / 10.5, 15.6 / 15.3, 22.2 / 21; 1024 x 1024 x 16384, tiles of 64, 4 ways 25.3 / 23.3, one way 39 / 43.
+double estimate(int side, int splits, double tiles, double stages, double outputs, double bytes)
+{
+    const double n = tiles * splits;
+    const double stage = side == 64 ? std::max(0.40 + 0.00047 * n, 0.00086 * n) : side == 128 ? std::max(0.79, 0.0027 * n) : std::max(1.2, 0.0082 * n);
+    return 2.6 + stage * (stages / splits) + (splits > 1 ? 2.2 + splits * outputs * 8 / 5.2e6 : outputs * bytes / 5.2e6);
+}
+
 Plan plan_of(const hq_mx4_problem *p, int group)
 {
-    if (group != BY_CHUNKS && p->M <= 16 * (long)p->experts) return Plan{0, 1};
-    const long tiles = (long)tiles_of(p->M, 128) * tiles_of(p->N, 128) * (group == BY_CHUNKS ? p->experts : 1);
-    int splits = 1;
-    if (group != BY_ROWS) {
-        const long chunks = hq_mx4_chunks(p->K, 1) / p->experts;
-        while (tiles * splits < 512 && chunks / (splits * 2) >= 4) splits *= 2;
+    // Few rows: B is read once and the rows of A beside it, without LDS.  (Rows / tiles of 64, us: one product of K = 4096, N = 4096 16 rows
+    // 4.3 / 9, 32 rows 5.3 / 8.5, 64 rows 9.2 / 9.1.  By expert the count is known on the device only, its mean here: 64 experts of 4096 x 1024
+    // 128 rows 21.1 / 26.3, 512 rows 32.5 / 29.9; 8 experts of 1024 x 4096 32 rows 5.9 / 10.3, 128 rows 12.5 / 10.5; 2 experts 32 rows 5.1 / 10.4.)
+    const long experts = p->experts;
+    if (group == BY_ROWS && p->M < 8 * experts) return Plan{1, 1};
+    if (group != BY_CHUNKS && p->M <= 32) return Plan{p->M <= 16 ? 1 : 2, 1};
+    const double outputs = (double)p->M * p->N * (group == BY_CHUNKS ? experts : 1), bytes = (double)hq_mx4_type_bytes(p->out_type);
+    // (segments: half a unit more than their rows fill)
+    const double stages = group == BY_CHUNKS ? (double)p->K / (256.0 * experts) + 0.5 : (double)hq_mx4_chunks(p->K, 1);
+    Plan best = {64, 1};
+    double least = 1e30;
+    for (int side = 64; side <= 256; side *= 2) {
+        const double m = group == BY_ROWS ? (double)p->M / side + 0.5 * std::min<long>(experts, p->M) : (double)tiles_of(p->M, side);
+        const double tiles = m * tiles_of(p->N, side) * (group == BY_CHUNKS ? experts : 1);
+        for (int splits = 1; splits == 1 || (group != BY_ROWS && splits <= 16 && stages / splits >= 2); splits *= 2) {
+            const double us = estimate(side, splits, tiles, stages, outputs, bytes);
+            if (us < least) { least = us; best = Plan{side, splits}; }
+        }
     }
-    const long large = (long)tiles_of(p->M, 256) * tiles_of(p->N, 256) * (group == BY_CHUNKS ? p->experts : 1);
-    return Plan{splits == 1 && large >= 256 && !getenv("MX_SMALL") ? 256 : 128, splits};
+    return best;
 }
 
 size_t outputs_of(const hq_mx4_problem *p, int group)
@@ -408,32 +440,35 @@ template <int GROUP> int product(const hq_mx4_problem *p, const uint8_t *A, cons
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     if (plan.splits > 1) {
         if (!ws || ws_bytes < 4 * a.outputs * plan.splits || misaligned(ws, 16)) return HQ_E_WORKSPACE;
-        a.part = static_cast<float *>(ws);
+        a.out = ws;
+        a.out_type = HQ_FP32;
     }
     if constexpr (GROUP != BY_CHUNKS) {
-        if (plan.tile == 0) {
+        if (plan.side <= 2) {
             a.n_tiles = tiles_of(p->N, 16);
             const long blocks = (long)a.n_tiles * p->experts;
             if (blocks >= 0x7fffffffL) return HQ_E_BADSHAPE;
             int waves = 1;
             while (waves < 8 && waves < a.chunks) waves *= 2;
-            hipLaunchKernelGGL((mx4_row_kernel<1, GROUP>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
+            if (plan.side == 2) hipLaunchKernelGGL((mx4_row_kernel<2, GROUP>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
+            else                hipLaunchKernelGGL((mx4_row_kernel<1, GROUP>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
             return launch_status();
         }
     }
-    const int side = plan.tile;
+    const int side = plan.side;
     const int used = std::min(p->experts, p->M);
     a.m_tiles = GROUP == BY_ROWS ? (p->M - used) / side + used : tiles_of(p->M, side);
     a.n_tiles = tiles_of(p->N, side);
     const double blocks = (double)a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? p->experts : 1) * a.splits;
     if (blocks >= 2147483648.0) return HQ_E_BADSHAPE;
-    rc = side == 256 ? launch_tile<256, 256, 4, 2, GROUP>(a, (long)blocks, s) : launch_tile<128, 128, 2, 2, GROUP>(a, (long)blocks, s);
+    rc = side == 256 ? launch_tile<256, 256, 4, 2, GROUP>(a, (long)blocks, s)
+       : side == 128 ? launch_tile<128, 128, 2, 2, GROUP>(a, (long)blocks, s) : launch_tile<64, 64, 2, 1, GROUP>(a, (long)blocks, s);
     if (rc != HQ_OK || a.splits == 1) return rc;
-    const unsigned join = (unsigned)std::min<size_t>((a.outputs / 4 + HQ_THREADS) / HQ_THREADS, 2048);
+    const float *part = static_cast<const float *>(ws);
     switch (p->out_type) {
-    case HQ_FP32: hipLaunchKernelGGL(mx4_join_kernel<HQ_FP32>, dim3(join), dim3(HQ_THREADS), 0, s, a.part, a.outputs, a.splits, out); break;
-    case HQ_BF16: hipLaunchKernelGGL(mx4_join_kernel<HQ_BF16>, dim3(join), dim3(HQ_THREADS), 0, s, a.part, a.outputs, a.splits, out); break;
-    default:      hipLaunchKernelGGL(mx4_join_kernel<HQ_FP16>, dim3(join), dim3(HQ_THREADS), 0, s, a.part, a.outputs, a.splits, out); break;
+    case HQ_FP32: launch_join<HQ_FP32>(part, a.outputs, a.splits, out, s); break;
+    case HQ_BF16: launch_join<HQ_BF16>(part, a.outputs, a.splits, out, s); break;
+    default:      launch_join<HQ_FP16>(part, a.outputs, a.splits, out, s); break;
     }
     return launch_status();
 }
