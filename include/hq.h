@@ -380,7 +380,7 @@ int64_t hq_mx4_chunks(int64_t n, int32_t segments);
  * Per block, amax = largest magnitude: scale 2^(floor(log2 amax) - 2), not below 2^-127 (byte 0, also for an all-zero block);
  * codes = x / scale to nearest, ties to the even code, magnitudes above 6 to 6.  A block with an infinity or a
  * NaN gets scale byte 255 and codes 0.  rows may be 0 (nothing is launched).
- * chunks(cols) * chunks(rows) * batch stays below 2^31, cols and rows below 2^31 - 256.                         */
+ * rows and cols stay below 2^31 - 256 (and a launch below 2^31 workgroups, which no tensor that fits the memory reaches). */
 int hq_mx4_quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
                     uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream);
 

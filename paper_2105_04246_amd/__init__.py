@@ -291,12 +291,17 @@ def mx4_problem(M, N, K, experts=1, out_type=HQ_FP32):
     return hq_mx4_problem(M, N, K, experts, out_type)
 
 
+_mx4_types = {}
+
+
 def mx4_type(dtype):
     """HQ_FP32, HQ_BF16 or HQ_FP16 of a torch dtype."""
-    types = {"torch.float32": HQ_FP32, "torch.bfloat16": HQ_BF16, "torch.float16": HQ_FP16}
-    if str(dtype) not in types:
+    if not _mx4_types:
+        import torch
+        _mx4_types.update({torch.float32: HQ_FP32, torch.bfloat16: HQ_BF16, torch.float16: HQ_FP16})
+    if dtype not in _mx4_types:
         raise ValueError("MX4 takes torch.float32, bfloat16 and float16, not %s" % dtype)
-    return types[str(dtype)]
+    return _mx4_types[dtype]
 
 
 def new_mx4(rows, n, segments=1, batch=1, device="cuda"):

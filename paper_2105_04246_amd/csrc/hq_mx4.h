@@ -6,7 +6,7 @@ typedef int v2i __attribute__((ext_vector_type(2)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int HqUnaligned16 __attribute__((ext_vector_type(4), aligned(2)));           // 16 bytes of a tensor at any element
 
 constexpr int MX_CHUNK = HQ_MX4_CHUNK, MX_CODES = HQ_MX4_CHUNK / 2, MX_SCALES = HQ_MX4_CHUNK / HQ_MX4_BLOCK;   // values, bytes, bytes
 constexpr long MX_MOST = 0x7fffffffL - MX_CHUNK;                          // rows, columns, products' sizes

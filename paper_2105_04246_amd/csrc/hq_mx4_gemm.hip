@@ -40,8 +40,6 @@ template <int SCALE_BYTE> __device__ inline v4f mfma16(v4i a, v4i b, v4f c, int 
 // wait states that the matrix pipe needs before its registers are read (it puts them before the second store).
 __device__ inline void mfma16_done(v4f &c) { asm volatile("s_nop 15" : "+v"(c)); }
 
-typedef int HqUnaligned16 __attribute__((ext_vector_type(4), aligned(2)));
-
 // COUNT consecutive outputs from column n on, of N, to `dst` (the address of column n); rounded once.
 template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const float *v, int n, int N)
 {
