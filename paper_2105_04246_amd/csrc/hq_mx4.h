@@ -68,7 +68,7 @@ template <int SIZE> __device__ inline HqSegment hq_segment_of(const int *offs, i
         if (e < segments) { lo = hq_segment_bound(offs, e, n); hi = max(lo, hq_segment_bound(offs, e + 1, n)); }
         const int units = (int)(((unsigned)(hi - lo) + SIZE - 1) / SIZE);
         const int upto = before + hq_wave_scan(units), mine = upto - units;
-        const unsigned long long hit = __builtin_amdgcn_ballot_w64(index >= mine && index < upto);
+        const unsigned long long hit = __builtin_amdgcn_ballot_w64((unsigned)(index - mine) < (unsigned)units);
         if (hit) {
             const int src = __builtin_ctzll(hit);
             return HqSegment{base + src, index - __builtin_amdgcn_readlane(mine, src), __builtin_amdgcn_readlane(lo, src),

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = lane >> 4, r16 = lane & 15, wm = wave / WN, wn = wave % WN;
 
-    // ---- which tile: each XCD takes a run of them, in bands of 8 row tiles
+    // ---- which tile: each XCD takes a run of them, in bands of row tiles
     const int per_split = a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? a.experts : 1);
     const int split = blockIdx.x / per_split;
     int tile = blockIdx.x - split * per_split;
@@ -100,8 +100,10 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
             }
         } else { e = b / mn; tile = b - e * mn; }
     }
-    const int band = tile / (8 * a.n_tiles), in_band = min(8, a.m_tiles - 8 * band), rest = tile - band * 8 * a.n_tiles;
-    const int tile_n = rest / in_band, tile_m = 8 * band + rest - tile_n * in_band;
+    // (tiles that run on an XCD together share operand panels: 4 x 8 of the largest.  8192 x 4096 x 4096 in bands of 8: 72 us, of 4: 68)
+    constexpr int BAND = BM == 256 ? 4 : 8;
+    const int band = tile / (BAND * a.n_tiles), in_band = min(BAND, a.m_tiles - BAND * band), rest = tile - band * BAND * a.n_tiles;
+    const int tile_n = rest / in_band, tile_m = BAND * band + rest - tile_n * in_band;
 
     int m0 = tile_m * BM, m_end = a.M, chunk0 = 0, nst = a.chunks;
     const int n0 = tile_n * BN;
@@ -237,6 +239,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
     for (; s + 2 < nst; s++) stage(std::true_type(), std::true_type());
     if (s + 1 < nst) { stage(std::false_type(), std::true_type()); s++; }
     if (s < nst) stage(std::false_type(), std::false_type());
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                       // (has been waited for: no wavefront ends with a load into LDS under way)
 
     // ---- a lane's columns of a row, 16 bytes at a time
     auto finish = [&](auto type, void *out) __attribute__((always_inline)) {
@@ -372,12 +375,13 @@ int tiles_of(long n, int side) { return (int)((n + side - 1) / side); }
 
 // Microseconds that a launch takes, so that tile and split can be chosen: a start, the stages of a workgroup, and the bytes of the outputs.  A
 // stage takes its latency while the compute units hold all workgroups at once, from there on their share of the card.  Fitted to (this / measured, us)
-// 1024 x 4096 x 4096 to bf16 in tiles of 64, 128, 256: 18.3 / 16.7, 16.9 / 17.0, 23.4 / 23.2; 4096 x 4096 x 4096 64.3 / 62.0, 53.4 / 48.0,
-// 42.6 / 35.6; 256 x 4096 x 4096 11.3 / 10.5, 15.6 / 15.3, 22.2 / 21; 1024 x 1024 x 16384, tiles of 64, 4 ways 25.3 / 23.3, one way 39 / 43.
+// products to bf16 in tiles of 64, 128, 256: 256 x 4096 x 4096 11.3 / 10.5, 15.6 / 15.3, 20 / 22; 1024 x 4096 x 4096 18.3 / 16.7, 16.9 / 17.0,
+// 24.3 / 23.2; 2048 x 4096 x 4096 34 / 33, 27.9 / 24.7, 30.0 / 25.7; 4096 x 4096 x 4096 65 / 62, 53 / 48, 43 / 36; 1024 x 1024 x 16384 four ways
+// 25.4 / 23.3, 23.9 / 24.1, 31.3 / 30.3, one way 37 / 43, 54 / 60, 72 / 85.
 double estimate(int side, int splits, double tiles, double stages, double outputs, double bytes)
 {
     const double n = tiles * splits;
-    const double stage = side == 64 ? std::max(0.40 + 0.00047 * n, 0.00086 * n) : side == 128 ? std::max(0.79, 0.0027 * n) : std::max(1.2, 0.0082 * n);
+    const double stage = side == 64 ? std::max(0.40 + 0.00047 * n, 0.00086 * n) : side == 128 ? std::max(0.79, 0.0027 * n) : std::max(1.0 + 0.0040 * n, 0.0082 * n);
     return 2.6 + stage * (stages / splits) + (splits > 1 ? 2.2 + splits * outputs * 8 / 5.2e6 : outputs * bytes / 5.2e6);
 }
 

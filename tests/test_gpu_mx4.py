@@ -133,6 +133,33 @@ def test_ragged_segments(counts, before, behind, seed):
     assert np.array_equal(back.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("counts", [None, [1500, 0, 2311, 255, 34], "batch"])
+@pytest.mark.parametrize("dtype,rows,cols", [("fp32", 4100, 2050), ("fp32", 4101, 2057), ("bf16", 4130, 4100), ("fp16", 4103, 4099)])
+def test_one_reading_of_a_large_tensor_gives_what_each_direction_gives(dtype, rows, cols, counts):
+    """From 32 MB on both directions come from one reading (tests/test_mx4_kernels.py); each alone comes from the kernel that the other tests hold to
+    the oracle."""
+    g = torch.Generator(device="cuda").manual_seed(rows + cols)
+    batch, offs, segments = 1, None, 1
+    if counts == "batch":
+        batch, rows = 4, rows // 4
+    elif counts:
+        segments = len(counts)
+        offs = offsets(counts)[1]
+    x = torch.randn((batch, rows, cols), generator=g, device="cuda") * torch.exp2(torch.randint(-12, 6, (batch, rows, cols), generator=g, device="cuda").float())
+    x.view(-1)[torch.randint(0, x.numel(), (200,), generator=g, device="cuda")] = float("nan")
+    x.view(-1)[torch.randint(0, x.numel(), (200,), generator=g, device="cuda")] = float("inf")
+    x = x.to(TYPES[dtype])
+    assert x.numel() * x.element_size() >= 32 << 20
+    q, qt = (containers(rows, cols, batch=batch), containers(cols, rows, segments, batch))
+    one, two = (containers(rows, cols, batch=batch), containers(cols, rows, segments, batch))
+    n = segments if counts and counts != "batch" else batch
+    quantize(x, rows, cols, n, offs, None, *q, *qt)
+    quantize(x, rows, cols, n, offs, None, *one, None, None)
+    quantize(x, rows, cols, n, offs, None, None, None, *two)
+    for a, b in zip(q + qt, one + two):
+        assert torch.equal(a, b)
+
+
 def special_blocks(dtype):
     """Blocks of 32 where a conversion can go wrong."""
     top, tiny = torch.finfo(dtype).max, torch.finfo(dtype).smallest_normal
@@ -284,6 +311,16 @@ def test_product(M, N, K, dtype):
     check(gemm(M, N, K, TYPES[dtype], dev(A), dev(B)), want, size, -(-K // 32), TYPES[dtype], "product")
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("M,N,K", [(1030, 4100, 700), (4100, 4133, 300), (1000, 1003, 16000), (3300, 3050, 4000)])
+def test_product_in_the_larger_tiles(M, N, K, dtype):
+    """Tiles of 128, of 256, of 128 with split sums, of 256 over many stages (tests/test_mx4_kernels.py holds these sizes to them), all with edges."""
+    rng = np.random.default_rng(M)
+    A, B = ([t[0] for t in random_container(rng, r, K)] for r in (M, N))
+    want, size = mx4.product(A, B)
+    check(gemm(M, N, K, TYPES[dtype], dev(A), dev(B)), want, size, -(-K // 32), TYPES[dtype], "product")
+
+
 @pytest.mark.parametrize("M,N,K", [(3, 20, 700), (150, 140, 700), (128, 128, 4096)])
 def test_product_with_scales_far_apart_and_blocks_that_are_not_numbers(M, N, K):
     rng = np.random.default_rng(3)
@@ -311,9 +348,11 @@ def test_product_of_nothing_is_zero():
 COUNTS = [[1], [0, 1, 0], [3, 0, 5, 16, 17], [130, 0, 1, 128, 127], [300, 0, 0, 2], [0, 0], [1] * 80, [400, 300]]
 
 
+BY_EXPERT = [(c, N, K) for c in COUNTS for N, K in ((40, 100), (130, 520))] + [([700, 0, 1100, 1290], 1100, 600), ([1500, 2200, 0, 500], 4100, 520)]
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("counts", COUNTS)
-@pytest.mark.parametrize("N,K", [(40, 100), (130, 520)])
+@pytest.mark.parametrize("counts,N,K", BY_EXPERT)
 def test_products_by_expert(counts, N, K, dtype):
     before, behind, E = 2, 3, len(counts)
     T = before + sum(counts) + behind
@@ -335,8 +374,8 @@ def test_products_by_expert(counts, N, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("counts", COUNTS + [[5000, 0, 700]])
-@pytest.mark.parametrize("M,N", [(40, 24), (130, 200)])
+@pytest.mark.parametrize("counts,M,N", [(c, M, N) for c in COUNTS + [[5000, 0, 700]] for M, N in ((40, 24), (130, 200))] +
+                         [([300, 0, 900, 513], 1030, 1100), ([300, 0, 1200], 4100, 2060)])
 def test_weight_gradients_by_expert(counts, M, N, dtype):
     E, T = len(counts), sum(counts)
     before, behind = (1, 2) if T < 1000 else (0, 0)

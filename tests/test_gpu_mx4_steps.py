@@ -1,0 +1,226 @@
+"""Microscaled 4-bit operators together, as a training step of a layer of experts and a serving step use them, on other streams and in
+captured graphs.  Integers whose magnitudes are on the 4-bit grid are quantized without a rounding in any block, and their products
+are exact in fp32, so every result has to equal the integers'."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2105_04246_amd as hq
+
+pytestmark = pytest.mark.gpu
+
+
+def integers(rng, shape, values=(0, 1, 2, 3, 4, 6)):
+    return (rng.choice(values, shape) * rng.choice((-1, 1), shape)).astype(np.float64)
+
+
+def dev(a, dtype=torch.float32):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(dtype).cuda()
+
+
+def offsets(counts):
+    o = np.concatenate([[0], np.cumsum(counts)])
+    return o, torch.tensor(o, dtype=torch.int32, device="cuda")
+
+
+class Experts:
+    """A layer W [experts][N][K] on T rows sorted by expert: buffers, and one step on them."""
+
+    def __init__(self, counts, N, K, dtype=torch.float32, stochastic=False):
+        self.counts, self.N, self.K, self.E, self.T = counts, N, K, len(counts), int(sum(counts))
+        self.o, self.offs = offsets(counts)
+        self.type, self.dtype, self.stochastic = hq.mx4_type(dtype), dtype, stochastic
+        T, E = self.T, self.E
+        self.X, self.G = (torch.zeros((T, n), dtype=dtype, device="cuda") for n in (K, N))
+        self.W = torch.zeros((E, N, K), dtype=dtype, device="cuda")
+        self.xq, self.xt = hq.new_mx4(T, K), hq.new_mx4(K, T, E)
+        self.gq, self.gt = hq.new_mx4(T, N), hq.new_mx4(N, T, E)
+        self.wq, self.wt = hq.new_mx4(N, K, batch=E), hq.new_mx4(K, N, batch=E)
+        self.Y, self.dX = torch.zeros((T, N), device="cuda"), torch.zeros((T, K), device="cuda")
+        self.dW = torch.zeros((E, N, K), device="cuda")
+        self.p_f, self.p_d = hq.mx4_problem(T, N, K, E), hq.mx4_problem(T, K, N, E)
+        self.p_w = hq.mx4_problem(N, K, T, E)
+        self.need = hq.hq_mx4_workspace_bytes(hq.HQ_ENTRY_MX4_WGRAD_GROUPED, self.p_w)
+        self.ws = torch.empty(max(16, self.need), dtype=torch.uint8, device="cuda")
+
+    def set(self, X, W, G):
+        for t, v in ((self.X, X), (self.W, W), (self.G, G)):
+            t.copy_(torch.from_numpy(np.ascontiguousarray(v)).to(self.dtype))
+
+    def step(self, stream=None):
+        hq.hq_mx4_quantize(self.type, self.W, self.N, self.K, self.E, None, *self.wq, *self.wt, stream=stream)
+        hq.hq_mx4_quantize(self.type, self.X, self.T, self.K, self.E, self.offs, *self.xq, *self.xt, stream=stream)
+        hq.hq_mx4_gemm_grouped(self.p_f, *self.xq, *self.wq, self.offs, self.Y, stream=stream)
+        if self.stochastic:
+            hq.hq_mx4_quantize_sr(self.type, self.G, self.T, self.N, self.E, self.offs, 3, *self.gq, *self.gt, stream=stream)
+        else:
+            hq.hq_mx4_quantize(self.type, self.G, self.T, self.N, self.E, self.offs, *self.gq, *self.gt, stream=stream)
+        hq.hq_mx4_gemm_grouped(self.p_d, *self.gq, *self.wt, self.offs, self.dX, stream=stream)
+        hq.hq_mx4_wgrad_grouped(self.p_w, *self.gt, *self.xt, self.offs, self.dW, self.ws, self.need, stream=stream)
+
+    def results(self):
+        torch.cuda.synchronize()
+        return [t.double().cpu().numpy() for t in (self.Y, self.dX, self.dW)]
+
+    def expected(self, X, W, G):
+        Y, dX, dW = np.zeros((self.T, self.N)), np.zeros((self.T, self.K)), np.zeros((self.E, self.N, self.K))
+        for e in range(self.E):
+            r = slice(self.o[e], self.o[e + 1])
+            Y[r], dX[r], dW[e] = X[r] @ W[e].T, G[r] @ W[e], G[r].T @ X[r]
+        return [Y, dX, dW]
+
+
+def drawn(rng, L, **more):
+    return integers(rng, (L.T, L.K), **more), integers(rng, (L.E, L.N, L.K), **more), integers(rng, (L.T, L.N), **more)
+
+
+def equal(got, want, what):
+    for g, w, name in zip(got, want, ("Y", "dX", "dW")):
+        assert np.array_equal(g, w), "%s: %s differs in %d places" % (what, name, (g != w).sum())
+
+
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("counts,N,K", [([3, 0, 1, 7], 40, 33), ([260, 0, 31, 129], 100, 70), ([700, 500, 0, 900], 300, 257), ([1] * 40, 64, 96),
+                                        ([5000, 3000], 128, 192)])
+def test_step_of_experts(counts, N, K, dtype, stochastic):
+    """On the grid stochastic rounding has nothing to round: the step is exact with it too."""
+    L = Experts(counts, N, K, dtype, stochastic)
+    data = drawn(np.random.default_rng(N), L)
+    L.set(*data)
+    L.step()
+    equal(L.results(), L.expected(*data), "step")
+
+
+def test_gradients_are_differences():
+    """loss = <Y, G> is linear in W and in X: its difference over W + D and W - D is twice <dW, D> exactly, and the same for X."""
+    rng = np.random.default_rng(4)
+    L = Experts([90, 0, 301, 18], 72, 100)
+    X, W, G = drawn(rng, L, values=(0, 2))
+    DX, DW, _ = drawn(rng, L, values=(0, 1))
+    L.set(X, W, G)
+    L.step()
+    _, dX, dW = L.results()
+
+    def loss(X, W):
+        L.set(X, W, G)
+        L.step()
+        return float((L.results()[0] * G).sum())
+    assert loss(X, W + DW) - loss(X, W - DW) == 2 * (dW * DW).sum() != 0
+    assert loss(X + DX, W) - loss(X - DX, W) == 2 * (dX * DX).sum() != 0
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 100, 300), (5, 64, 4096), (300, 200, 400), (600, 256, 8192)])
+def test_step_of_a_linear_layer(M, N, K):
+    """Forward, input gradient and weight gradient of one layer by hq_mx4_gemm, each with its own containers."""
+    rng = np.random.default_rng(M)
+    # (sums of up to 8192 products of at most 36 stay below 2^24)
+    X, W, G = (integers(rng, s) for s in ((M, K), (N, K), (M, N)))
+    x, w, g = dev(X, torch.bfloat16), dev(W), dev(G, torch.float16)
+    xq, xt, wq, wt, gq, gt = (hq.new_mx4(*s) for s in ((M, K), (K, M), (N, K), (K, N), (M, N), (N, M)))
+    hq.hq_mx4_quantize(hq.HQ_BF16, x, M, K, 1, None, *xq, *xt)
+    hq.hq_mx4_quantize(hq.HQ_FP32, w, N, K, 1, None, *wq, *wt)
+    hq.hq_mx4_quantize(hq.HQ_FP16, g, M, N, 1, None, *gq, *gt)
+    for A, B, m, n, k, want in ((xq, wq, M, N, K, X @ W.T), (gq, wt, M, K, N, G @ W), (gt, xt, N, K, M, G.T @ X)):
+        p = hq.mx4_problem(m, n, k)
+        need = hq.hq_mx4_workspace_bytes(hq.HQ_ENTRY_MX4_GEMM, p)
+        ws = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
+        out = torch.empty((m, n), device="cuda")
+        hq.hq_mx4_gemm(p, *A, *B, out, ws, need)
+        torch.cuda.synchronize()
+        assert np.array_equal(out.cpu().numpy(), want)
+
+
+def test_two_streams_at_once():
+    """Two steps with buffers of their own, interleaved call by call on two streams."""
+    rng = np.random.default_rng(5)
+    layers = [Experts([200, 0, 333], 128, 260), Experts([64, 900, 1], 200, 96)]
+    data = [drawn(rng, L) for L in layers]
+    for L, d in zip(layers, data):
+        L.set(*d)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for L, s in zip(layers, streams):
+            L.step(s)
+    for L, d in zip(layers, data):
+        equal(L.results(), L.expected(*d), "stream")
+
+
+def test_captured_step_replays_on_new_data():
+    """Two layers captured into graphs, replayed in turn with other inputs and other segments, eager work between the replays."""
+    rng = np.random.default_rng(6)
+    layers = [Experts([3000, 2500, 0], 64, 96), Experts([120, 0, 7], 130, 64)]
+    graphs = []
+    for L in layers:
+        L.set(*drawn(rng, L))
+        L.step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            L.step()
+        graphs.append(g)
+    eager = Experts([50, 60], 40, 50)
+    for turn in range(4):
+        for L, g in zip(layers, graphs):
+            data = drawn(rng, L)
+            L.set(*data)
+            cut = np.sort(rng.integers(0, L.T + 1, L.E - 1))
+            L.o = np.concatenate([[0], cut, [L.T]])
+            L.offs.copy_(torch.tensor(L.o, dtype=torch.int32))
+            g.replay()
+            torch.cuda.synchronize()
+            mixed = drawn(rng, eager)
+            eager.set(*mixed)
+            eager.step()
+            equal(eager.results(), eager.expected(*mixed), "eager, turn %d" % turn)
+            equal(L.results(), L.expected(*data), "replay, turn %d" % turn)
+
+
+def test_the_same_call_gives_the_same_bits():
+    rng = np.random.default_rng(7)
+    L = Experts([2000, 0, 1111, 5], 96, 320)
+    x, w, g = (rng.standard_normal(s) for s in ((L.T, L.K), (L.E, L.N, L.K), (L.T, L.N)))
+    L.set(x, w, g)
+    L.step()
+    first = L.results()
+    for t in (L.Y, L.dX, L.dW, L.ws):
+        t.fill_(77)
+    L.step()
+    equal(L.results(), first, "again")
+
+
+@pytest.mark.parametrize("values", [[0, 500, 100, 900], [-5, 10, 700, 5000], [300, 200, 100, 0], [2 ** 31 - 1, -2 ** 31, 0, 64], [64, 64, 64, 64]])
+def test_offsets_outside_their_limits_stay_inside_the_tensors(values):
+    """Clamped to 0 .. T, a descending pair is an empty segment: what follows from that is computed, and nothing beside the tensors is touched."""
+    T, N, K, E = 640, 96, 64, 3
+    rng = np.random.default_rng(8)
+    X, W = integers(rng, (T, K)), integers(rng, (E, N, K))
+    offs = torch.tensor(values, dtype=torch.int32, device="cuda")
+    pad = 4096
+    flat = [torch.full((n + 2 * pad,), 0xA5, dtype=torch.uint8, device="cuda") for n in
+            (T * 128, T * 8, hq.hq_mx4_chunks(T, E) * K * 128, hq.hq_mx4_chunks(T, E) * K * 8, 4 * T * N)]
+    q, s, qt, st, y = (f[pad:-pad] for f in flat)
+    y.zero_()
+    wq = hq.new_mx4(N, K, batch=E)
+    hq.hq_mx4_quantize(hq.HQ_FP32, dev(W), N, K, E, None, *wq, None, None)
+    hq.hq_mx4_quantize(hq.HQ_FP32, dev(X), T, K, 1, None, q, s, None, None)
+    hq.hq_mx4_quantize(hq.HQ_FP32, dev(X), T, K, E, offs, q, s, qt, st)
+    hq.hq_mx4_gemm_grouped(hq.mx4_problem(T, N, K, E), q, s, *wq, offs, y)
+    dw = torch.empty((E, K, K), device="cuda")
+    p = hq.mx4_problem(K, K, T, E)
+    need = hq.hq_mx4_workspace_bytes(hq.HQ_ENTRY_MX4_WGRAD_GROUPED, p)
+    hq.hq_mx4_wgrad_grouped(p, qt, st, qt, st, offs, dw, torch.empty(max(16, need), dtype=torch.uint8, device="cuda"), need)
+    torch.cuda.synchronize()
+    for f in flat:
+        assert bool((f[:pad] == 0xA5).all()) and bool((f[-pad:] == 0xA5).all())
+    lo = np.clip(values, 0, T)
+    got, covered = y.view(torch.float32).view(T, N).cpu().numpy(), np.zeros(T, int)
+    for e in range(E):
+        covered[lo[e]:max(lo[e], lo[e + 1])] += 1
+    if covered.max(initial=0) <= 1:                                       # segments that do not overlap have one meaning
+        want = np.zeros((T, N))
+        for e in range(E):
+            r = slice(lo[e], max(lo[e], lo[e + 1]))
+            want[r] = X[r] @ W[e].T
+        assert np.array_equal(got, want)
