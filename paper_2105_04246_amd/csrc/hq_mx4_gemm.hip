@@ -67,12 +67,13 @@ template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const
 // ---------------------------------------------------------------------------------------
 // Tiles of BM x BN outputs, WM x WN wavefronts of (BM / WM) x (BN / WN) each.  A stage is one chunk of the tile's rows of A and B, straight
 // from memory into one of two LDS buffers.  A step is half a chunk: one of a lane's two blocks of a row.  Tiles of 256 have 8 wavefronts of 64 x 128
-// (128 accumulator registers a lane, one workgroup to a compute unit), which read 192 KB of fragments a stage from LDS; tiles of 128 (4 wavefronts, two workgroups) and of 64 (2 wavefronts, four) fill the card where there are few.
+// (128 accumulator registers a lane, one workgroup to a compute unit), which read 192 KB of fragments a stage from LDS; tiles of 128 (4 wavefronts,
+// two workgroups) and of 64 (2 wavefronts, four) fill the card where there are few.
 // Measured: 8192 x 4096 x 4096 to bf16 65 us, 4.2 PFLOP/s (tiles of 128 86, of 64 121); the matrix pipes are busy for 46 % of the cycles at 2.07
-// GHz.  Without its loads the kernel takes 62 us, without its stores 60, without both and without products 48: what is left is the start of a tile
-// (two of them to a compute unit) and its stores, during which all compute units do the same.  Stages of half a chunk in a ring of four took 87 us,
-// one buffer and four workgroups of 128 x 128 102, a workgroup that keeps its place for many tiles and requests the next one's stages before
-// it stores 74; lines touched ahead of their loads 73.
+// GHz.  On a card where it took 70 us, it took 62 without its loads, 60 without its stores, 48 without loads and products: what is left is the start
+// of a tile (two of them to a compute unit) and its stores, during which all compute units do the same.  Slower (against 66 to 74 of the same day):
+// stages of half a chunk in a ring of four 87 us, one buffer and four workgroups of 128 x 128 102, workgroups that keep their place and request the
+// next tile's stages before they store 77, lines touched ahead of their loads 73.
 // Weight gradients of 16 experts, 4096 x 1024 fp32 over 16384 rows: 63 us, 268 MB written and 60 MB read from memory (5.2 TB/s, a copy's rate).
 // ---------------------------------------------------------------------------------------
 
