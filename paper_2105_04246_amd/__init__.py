@@ -309,8 +309,8 @@ def new_mx4(rows, n, segments=1, batch=1, device="cuda"):
     (0 or 1: one)."""
     import torch
     chunks = batch * hq_mx4_chunks(n, max(1, segments))
-    return (torch.empty((chunks, rows, HQ_MX4_CHUNK // 2), dtype=torch.uint8, device=device),
-            torch.empty((chunks, rows, HQ_MX4_CHUNK // HQ_MX4_BLOCK), dtype=torch.uint8, device=device))
+    return (torch.empty(chunks, rows, HQ_MX4_CHUNK // 2, dtype=torch.uint8, device=device),
+            torch.empty(chunks, rows, HQ_MX4_CHUNK // HQ_MX4_BLOCK, dtype=torch.uint8, device=device))
 
 
 def to_device(rec, device="cuda"):

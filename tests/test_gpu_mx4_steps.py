@@ -224,3 +224,49 @@ def test_offsets_outside_their_limits_stay_inside_the_tensors(values):
             r = slice(lo[e], max(lo[e], lo[e + 1]))
             want[r] = X[r] @ W[e].T
         assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [8, 40])
+def test_containers_beyond_4_gb(rows):
+    """All rows belong to the last expert, whose codes lie behind the first 4 GB: the same as one product with its part alone.  (Scales of 1: sums of at
+    most 8192 multiples of a quarter below 36 are exact in fp32, in any order.)"""
+    E, N, K = 9, 131072, 8192
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("needs 8 GB of free memory")
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    draw = lambda *s: torch.randint(0, 256, s, dtype=torch.uint8, generator=g, device="cuda")        # noqa: E731
+    chunks = hq.hq_mx4_chunks(K)
+    B, Bs = draw(E * chunks, N, 128), torch.full((E * chunks, N, 8), 127, dtype=torch.uint8, device="cuda")
+    A, As = draw(chunks, rows, 128), torch.full((chunks, rows, 8), 127, dtype=torch.uint8, device="cuda")
+    assert (E - 1) * chunks * N * 128 >= 1 << 32
+    offs = torch.tensor([0] * E + [rows], dtype=torch.int32, device="cuda")
+    got, want = (torch.empty((rows, N), device="cuda") for _ in range(2))
+    hq.hq_mx4_gemm_grouped(hq.mx4_problem(rows, N, K, E), A, As, B, Bs, offs, got)
+    p = hq.mx4_problem(rows, N, K)
+    need = hq.hq_mx4_workspace_bytes(hq.HQ_ENTRY_MX4_GEMM, p)
+    ws = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
+    last = (E - 1) * chunks
+    hq.hq_mx4_gemm(p, A, As, B[last:].clone(), Bs[last:].clone(), want, ws, need)
+    assert torch.equal(got, want) and bool(want.any())
+
+
+def test_outputs_beyond_2_to_the_32_elements():
+    """Two experts' weight gradients of 65536 x 40000 from a row each, in bf16 (10 GB): products of grid values, exact."""
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB of free memory")
+    M, N, E = 65536, 40000, 2
+    rng = np.random.default_rng(12)
+    g, x = integers(rng, (E, M)), integers(rng, (E, N))
+    offs = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    gt, xt = hq.new_mx4(M, E, E), hq.new_mx4(N, E, E)
+    hq.hq_mx4_quantize(hq.HQ_FP32, dev(g), E, M, E, offs, None, None, *gt)
+    hq.hq_mx4_quantize(hq.HQ_FP32, dev(x), E, N, E, offs, None, None, *xt)
+    p = hq.mx4_problem(M, N, E, E, hq.HQ_BF16)
+    need = hq.hq_mx4_workspace_bytes(hq.HQ_ENTRY_MX4_WGRAD_GROUPED, p)
+    out = torch.full((E, M, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+    assert out.numel() > 1 << 32
+    hq.hq_mx4_wgrad_grouped(p, *gt, *xt, offs, out, torch.empty(max(16, need), dtype=torch.uint8, device="cuda"), need)
+    for e in range(E):
+        gd, xd = dev(g[e], torch.bfloat16), dev(x[e], torch.bfloat16)
+        for rows in torch.arange(M, device="cuda").split(8192):
+            assert torch.equal(out[e, rows[0]:rows[-1] + 1], gd[rows][:, None] * xd[None])
