@@ -380,7 +380,8 @@ int64_t hq_mx4_chunks(int64_t n, int32_t segments);
  * Per block, amax = largest magnitude: scale 2^(floor(log2 amax) - 2), not below 2^-127 (byte 0, also for an all-zero block);
  * codes = x / scale to nearest, ties to the even code, magnitudes above 6 to 6.  A block with an infinity or a
  * NaN gets scale byte 255 and codes 0.  rows may be 0 (nothing is launched).
- * rows and cols stay below 2^31 - 256 (and a launch below 2^31 workgroups, which no tensor that fits the memory reaches). */
+ * rows and cols stay below 2^31 - 256, and a call, here as in the entry points below, below 2^31 pieces of work (here: 32 rows of up to 256
+ * columns along the rows, 256 rows of up to 64 columns along the columns, of a matrix or a segment); HQ_E_BADSHAPE otherwise. */
 int hq_mx4_quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
                     uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream);
 

@@ -14,6 +14,20 @@ constexpr long MX_MOST = 0x7fffffffL - MX_CHUNK;                          // row
 inline bool hq_mx4_type_ok(int type) { return type == HQ_FP32 || type == HQ_BF16 || type == HQ_FP16; }
 inline size_t hq_mx4_type_bytes(int type) { return type == HQ_FP32 ? 4 : 2; }
 
+// `blocks` workgroups of `threads` each, in as many launches as they need: HIP takes fewer than 2^32 threads in one.  launch(first, count): those from
+// number `first` on.  (Runs of a multiple of 8: a workgroup's number modulo 8 stays that of its XCD.)
+template <typename Launch> inline int hq_mx4_launch(unsigned blocks, unsigned threads, const Launch &launch)
+{
+    const unsigned most = 0xffffffffu / threads;
+    for (unsigned first = 0; first < blocks;) {
+        const unsigned left = blocks - first, count = left <= most ? left : most & ~7u;
+        launch(first, count);
+        if (hipGetLastError() != hipSuccess) return HQ_E_HIP;
+        first += count;
+    }
+    return HQ_OK;
+}
+
 // ---- real values -------------------------------------------------------------------------------
 // Rounded to nearest even where the type is narrower than fp32 (bf16, fp16: 2^-9 and 2^-12 relative at most).
 template <int TYPE> struct HqReal;

@@ -29,6 +29,7 @@ struct ProductArgs {
     int experts, splits;
     int m_tiles, n_tiles;
     int out_type;
+    unsigned first;                // the launch's first workgroup
 };
 
 template <int SCALE_BYTE> __device__ inline v4f mfma16(v4i a, v4i b, v4f c, int sa, int sb)
@@ -100,14 +101,15 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
 
     // ---- which tile: each XCD takes a run of them, in bands of row tiles
     const int per_split = a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? a.experts : 1);
-    const int split = blockIdx.x / per_split;
-    int tile = blockIdx.x - split * per_split;
+    const unsigned block = a.first + blockIdx.x;
+    const int split = block / per_split;
+    int tile = block - split * per_split;
     const int per = per_split / 8;
     if (tile < per * 8) tile = (tile & 7) * per + (tile >> 3);
     int e = 0;
     if (GROUP == BY_CHUNKS) {
         // (every expert's tiles over all XCDs: their contractions differ in length)
-        const int mn = a.m_tiles * a.n_tiles, share = mn / 8, b = blockIdx.x - split * per_split;
+        const int mn = a.m_tiles * a.n_tiles, share = mn / 8, b = block - split * per_split;
         if (share) {
             if (b < share * 8 * a.experts) {
                 const int x = b & 7, t = b >> 3;
@@ -297,8 +299,9 @@ template <int MT, int GROUP> __global__ __launch_bounds__(512) void mx4_row_kern
     __shared__ float sums[8][MT][16][17];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int r16 = lane & 15, group = lane >> 4;
-    const int e = GROUP == BY_ROWS ? blockIdx.x / a.n_tiles : 0;
-    const int n0 = (int)(blockIdx.x - (unsigned)e * (unsigned)a.n_tiles) * 16;
+    const unsigned block = a.first + blockIdx.x;
+    const int e = GROUP == BY_ROWS ? block / a.n_tiles : 0;
+    const int n0 = (int)(block - (unsigned)e * (unsigned)a.n_tiles) * 16;
     int m_first = 0, m_end = a.M;
     if (GROUP == BY_ROWS) {
         m_first = hq_segment_bound(a.offs, e, a.M);
@@ -437,13 +440,15 @@ size_t outputs_of(const hq_mx4_problem *p, int group)
     return (size_t)p->M * (size_t)p->N * (group == BY_CHUNKS ? (size_t)p->experts : 1);
 }
 
-template <int BM, int BN, int WM, int WN, int GROUP> int launch_tile(const ProductArgs &a, long blocks, hipStream_t s)
+template <int BM, int BN, int WM, int WN, int GROUP> int launch_tile(ProductArgs a, unsigned blocks, hipStream_t s)
 {
     const size_t lds = 2 * (BM + BN) * (MX_CODES + MX_SCALES);
     static std::atomic<unsigned long long> allowed{0};
     if (!hq_allow_lds(mx4_tile_kernel<BM, BN, WM, WN, GROUP>, lds, allowed)) return HQ_E_HIP;
-    hipLaunchKernelGGL((mx4_tile_kernel<BM, BN, WM, WN, GROUP>), dim3((unsigned)blocks), dim3(64 * WM * WN), lds, s, a);
-    return launch_status();
+    return hq_mx4_launch(blocks, 64 * WM * WN, [&](unsigned first, unsigned count) {
+        a.first = first;
+        hipLaunchKernelGGL((mx4_tile_kernel<BM, BN, WM, WN, GROUP>), dim3(count), dim3(64 * WM * WN), lds, s, a);
+    });
 }
 
 template <int GROUP> int product(const hq_mx4_problem *p, const uint8_t *A, const uint8_t *As, const uint8_t *B, const uint8_t *Bs,
@@ -475,9 +480,11 @@ template <int GROUP> int product(const hq_mx4_problem *p, const uint8_t *A, cons
             if (blocks >= 0x7fffffffL) return HQ_E_BADSHAPE;
             int waves = 1;
             while (waves < 8 && waves < a.chunks) waves *= 2;
-            if (plan.side == 2) hipLaunchKernelGGL((mx4_row_kernel<2, GROUP>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
-            else                hipLaunchKernelGGL((mx4_row_kernel<1, GROUP>), dim3((unsigned)blocks), dim3(64 * waves), 0, s, a);
-            return launch_status();
+            return hq_mx4_launch((unsigned)blocks, 64 * waves, [&](unsigned first, unsigned count) {
+                a.first = first;
+                if (plan.side == 2) hipLaunchKernelGGL((mx4_row_kernel<2, GROUP>), dim3(count), dim3(64 * waves), 0, s, a);
+                else                hipLaunchKernelGGL((mx4_row_kernel<1, GROUP>), dim3(count), dim3(64 * waves), 0, s, a);
+            });
         }
     }
     const int side = plan.side;
@@ -486,8 +493,8 @@ template <int GROUP> int product(const hq_mx4_problem *p, const uint8_t *A, cons
     a.n_tiles = tiles_of(p->N, side);
     const double blocks = (double)a.m_tiles * a.n_tiles * (GROUP == BY_CHUNKS ? p->experts : 1) * a.splits;
     if (blocks >= 2147483648.0) return HQ_E_BADSHAPE;
-    rc = side == 256 ? launch_tile<256, 256, 4, 2, GROUP>(a, (long)blocks, s)
-       : side == 128 ? launch_tile<128, 128, 2, 2, GROUP>(a, (long)blocks, s) : launch_tile<64, 64, 2, 1, GROUP>(a, (long)blocks, s);
+    rc = side == 256 ? launch_tile<256, 256, 4, 2, GROUP>(a, (unsigned)blocks, s)
+       : side == 128 ? launch_tile<128, 128, 2, 2, GROUP>(a, (unsigned)blocks, s) : launch_tile<64, 64, 2, 1, GROUP>(a, (unsigned)blocks, s);
     if (rc != HQ_OK || a.splits == 1) return rc;
     const float *part = static_cast<const float *>(ws);
     switch (p->out_type) {

@@ -31,6 +31,7 @@ struct QuantizeArgs {
     int kc;                                        // chunks along the columns' axis (of a row)
     int tiles_rows, tiles_cols;                    // row tiles of a matrix (without offs) of the workgroups along the rows, along the columns
     unsigned first_cols;                           // first workgroup along the columns, where they are others
+    unsigned first;                                // the launch's first workgroup
     HqSr sr;
 };
 
@@ -287,14 +288,15 @@ template <int CPL> constexpr int MQ_LDS_COLS = 64 * CPL * (MQ_PITCH + MX_SCALES)
 template <int TYPE> __global__ __launch_bounds__(64 * MQ_WAVES) void mx4_quantize_kernel(const QuantizeArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[MQ_LDS_COLS<4> + MQ_WAVES * 32 * MX_SCALES];
-    quantize_piece<TYPE, true, true, false, 32, 4>(a, blockIdx.x, lds);
+    quantize_piece<TYPE, true, true, false, 32, 4>(a, a.first + blockIdx.x, lds);
 }
 // Each direction by workgroups of its own: along the rows up to a.first_cols, along the columns from there on.
 template <int TYPE, bool SR> __global__ __launch_bounds__(64 * MQ_WAVES) void mx4_quantize_pieces_kernel(const QuantizeArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[MQ_LDS_COLS<1>];
-    if (blockIdx.x < a.first_cols) quantize_piece<TYPE, true, false, SR, 4, 4>(a, blockIdx.x, lds);
-    else                           quantize_piece<TYPE, false, true, SR, 32, 1>(a, blockIdx.x - a.first_cols, lds);
+    const unsigned block = a.first + blockIdx.x;
+    if (block < a.first_cols) quantize_piece<TYPE, true, false, SR, 4, 4>(a, block, lds);
+    else                      quantize_piece<TYPE, false, true, SR, 32, 1>(a, block - a.first_cols, lds);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -305,6 +307,7 @@ struct DequantizeArgs {
     int rows, n, segments;
     int chunks;                                    // of a matrix (without offs)
     int tiles;                                     // row tiles
+    unsigned first;                                // the launch's first workgroup
 };
 
 template <int TYPE> constexpr int MD_ROWS = TYPE == HQ_FP32 ? 8 : 16;        // rows of a workgroup, in two turns; a lane writes 16 bytes of a row
@@ -312,8 +315,8 @@ template <int TYPE> constexpr int MD_ROWS = TYPE == HQ_FP32 ? 8 : 16;        // 
 template <int TYPE> __global__ __launch_bounds__(HQ_THREADS) void mx4_dequantize_kernel(const DequantizeArgs a)
 {
     typedef typename HqReal<TYPE>::T T;
-    const unsigned y = blockIdx.x / (unsigned)a.tiles;
-    const int tile = (int)(blockIdx.x - y * (unsigned)a.tiles);
+    const unsigned block = a.first + blockIdx.x, y = block / (unsigned)a.tiles;
+    const int tile = (int)(block - y * (unsigned)a.tiles);
     int k0, valid;                                 // the chunk's place on the axis, its values
     size_t matrix = 0;
     if (a.offs) {
@@ -357,15 +360,16 @@ template <int TYPE> __global__ __launch_bounds__(HQ_THREADS) void mx4_dequantize
 }
 
 inline bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-inline int launch_status() { return hipGetLastError() == hipSuccess ? HQ_OK : HQ_E_HIP; }
 
-template <int TYPE> int launch_quantize(const QuantizeArgs &a, bool pieces, bool sr, unsigned blocks, hipStream_t s)
+template <int TYPE> int launch_quantize(QuantizeArgs a, bool pieces, bool sr, unsigned blocks, hipStream_t s)
 {
-    const dim3 grid(blocks), threads(64 * MQ_WAVES);
-    if (!pieces) hipLaunchKernelGGL(mx4_quantize_kernel<TYPE>, grid, threads, 0, s, a);
-    else if (sr) hipLaunchKernelGGL((mx4_quantize_pieces_kernel<TYPE, true>), grid, threads, 0, s, a);
-    else         hipLaunchKernelGGL((mx4_quantize_pieces_kernel<TYPE, false>), grid, threads, 0, s, a);
-    return launch_status();
+    constexpr unsigned threads = 64 * MQ_WAVES;
+    return hq_mx4_launch(blocks, threads, [&](unsigned first, unsigned count) {
+        a.first = first;
+        if (!pieces) hipLaunchKernelGGL(mx4_quantize_kernel<TYPE>, dim3(count), dim3(threads), 0, s, a);
+        else if (sr) hipLaunchKernelGGL((mx4_quantize_pieces_kernel<TYPE, true>), dim3(count), dim3(threads), 0, s, a);
+        else         hipLaunchKernelGGL((mx4_quantize_pieces_kernel<TYPE, false>), dim3(count), dim3(threads), 0, s, a);
+    });
 }
 
 int quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs, const uint64_t *seed,
@@ -441,14 +445,16 @@ int hq_mx4_dequantize(const uint8_t *Q, const uint8_t *S, int32_t rows, int32_t 
     if ((double)y * a.tiles >= 2147483648.0) return HQ_E_BADSHAPE;
     if (y == 0 || a.tiles == 0) return HQ_OK;
     if (!Q || !S || !X) return HQ_E_BADARG;
-    const dim3 grid((unsigned)(y * a.tiles)), threads(HQ_THREADS);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    switch (xtype) {
-    case HQ_FP32: hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_FP32>, grid, threads, 0, s, a); break;
-    case HQ_BF16: hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_BF16>, grid, threads, 0, s, a); break;
-    default:      hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_FP16>, grid, threads, 0, s, a); break;
-    }
-    return launch_status();
+    return hq_mx4_launch((unsigned)(y * a.tiles), HQ_THREADS, [&](unsigned first, unsigned count) {
+        a.first = first;
+        const dim3 grid(count), threads(HQ_THREADS);
+        switch (xtype) {
+        case HQ_FP32: hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_FP32>, grid, threads, 0, s, a); break;
+        case HQ_BF16: hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_BF16>, grid, threads, 0, s, a); break;
+        default:      hipLaunchKernelGGL(mx4_dequantize_kernel<HQ_FP16>, grid, threads, 0, s, a); break;
+        }
+    });
 }
 
 } // extern "C"
