@@ -28,7 +28,9 @@ elif op == "dequantize":
     hq.hq_mx4_dequantize(P, P, rows, n, batch, None, type, P, 0)
 else:
     p = hq.mx4_problem(*args)
-    if op == "rows":
+    if op == "gemm":
+        hq.hq_mx4_gemm(p, P, P, P, P, P, P, 1 << 40, 0)
+    elif op == "rows":
         hq.hq_mx4_gemm_grouped(p, P, P, P, P, P, P, 0)
     else:
         hq.hq_mx4_wgrad_grouped(p, P, P, P, P, P, P, P, 1 << 40, 0)
@@ -63,12 +65,16 @@ CASES = [
 ]
 
 
+def launched(op, args):
+    r = subprocess.run([sys.executable, "-c", CHILD, launches.recorder(), ROOT], input=json.dumps((op, args)), capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[-2000:]
+    return json.loads(r.stdout)
+
+
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(v) for v in (c[0],) + c[1]))
 def test_launches_stay_below_their_limit(case):
     op, args, kernel, blocks, threads = case
-    r = subprocess.run([sys.executable, "-c", CHILD, launches.recorder(), ROOT], input=json.dumps((op, args)), capture_output=True, text=True, timeout=120)
-    assert r.returncode == 0, r.stderr[-2000:]
-    got = json.loads(r.stdout)
+    got = launched(op, args)
     assert got
     runs = [int(l[1]) for l in got]
     for l in got:
@@ -77,3 +83,22 @@ def test_launches_stay_below_their_limit(case):
     assert all(n % 8 == 0 for n in runs[:-1])
     assert blocks is None or sum(runs) == blocks
     assert (len(runs) == 1) == (sum(runs) * threads < LIMIT)
+
+
+# ---- which kernels the sizes of the GPU tests take
+
+TILE = "mx4_tile_kernel<%d, %d, "
+SPLIT = [([12000, 0, 200], 3, 65, 67, 64, 1), ([16000, 300, 0], 3, 130, 200, 64, 4), ([16000, 1, 0, 255], 4, 65, 68, 64, 4),
+         ([0, 5000, 0, 11111], 3, 64, 128, 64, 4), ([14000, 2384], 0, 510, 1022, 128, 4), ([16000, 381], 6, 509, 1021, 128, 1),
+         ([12000, 0, 200], 0, 64, 96, 64, 4), ([300, 15000, 1], 0, 130, 64, 64, 4), ([7000, 5100, 0], 0, 40, 50, 64, 4)]
+
+
+@pytest.mark.parametrize("counts,beside,M,N,side,width", SPLIT)
+@pytest.mark.parametrize("out", (0, 1, 2))
+def test_weight_gradients_that_split(counts, beside, M, N, side, width, out):
+    """Sizes of tests/test_gpu_mx4_split.py: more parts than the shortest segments have chunks, joined 4 outputs at a time or one by one."""
+    E = len(counts)
+    got = launched("wgrad", (M, N, sum(counts) + beside, E, out))
+    assert [l[0].startswith(w) for l, w in zip(got, (TILE % (side, side), "mx4_join_kernel<%d, %d" % (out, width)))] == [True, True] and len(got) == 2
+    parts = int(got[0][1]) // (-(-M // side) * -(-N // side) * E)
+    assert parts >= 2 and (E == 2 or any(-(-n // 256) < parts for n in counts))
