@@ -102,3 +102,12 @@ def test_weight_gradients_that_split(counts, beside, M, N, side, width, out):
     assert [l[0].startswith(w) for l, w in zip(got, (TILE % (side, side), "mx4_join_kernel<%d, %d" % (out, width)))] == [True, True] and len(got) == 2
     parts = int(got[0][1]) // (-(-M // side) * -(-N // side) * E)
     assert parts >= 2 and (E == 2 or any(-(-n // 256) < parts for n in counts))
+
+
+def test_kernels_of_operands_beyond_4_gb():
+    """Sizes of tests/test_gpu_mx4_far.py."""
+    for op, args, side in (("rows", (72, 131072, 8192, 9, 0), 64), ("rows", (2000, 131072, 8192, 9, 0), 256), ("gemm", (40, 1 << 22, 9 * 256, 1, 0), 64),
+                           ("gemm", (300, 1 << 22, 9 * 256, 1, 0), 128), ("wgrad", (1 << 22, 40, 2560, 2, 0), 64),
+                           ("wgrad", (1 << 22, 300, 2560, 2, 0), 128)):
+        got = launched(op, args)
+        assert len(got) == 1 and got[0][0].startswith(TILE % (side, side)), (op, args, got)
