@@ -354,7 +354,8 @@ int hq_tensor_quantize_dynamic(int32_t mode, const float *X, size_t n, hq_range 
  * and what an entry point would write for them is left as it was.  (The library cannot refuse values on the
  * device: they are clamped to 0 .. n and a descending pair is an empty segment.)
  *
- * Q, S, X and out are 16-byte aligned; types of real-valued tensors are HQ_FP32, HQ_BF16, HQ_FP16.
+ * Q, S, X and out are 16-byte aligned; types of real-valued tensors are HQ_FP32, HQ_BF16, HQ_FP16.  (Matrix e of a batch of containers
+ * begins at byte 8 * e * chunks * rows of S: where that is no multiple of 16, its scales have to be copied for a call of their own.)
  * ------------------------------------------------------------------------------------------- */
 #define HQ_FP32 0
 #define HQ_BF16 1
@@ -369,8 +370,8 @@ int hq_tensor_quantize_dynamic(int32_t mode, const float *X, size_t n, hq_range 
  * the most that any distribution of the values over the segments needs. */
 int64_t hq_mx4_chunks(int64_t n, int32_t segments);
 
-/* Quantizes a real-valued matrix into containers along its rows, along its columns, or both in one
- * reading of X: a layer's forward product sums over one axis of a tensor, its gradients over the other.
+/* Quantizes a real-valued matrix into containers along its rows, along its columns, or both in one call (from 32 MB on in one reading of X; below
+ * that, and stochastically, in two): a layer's forward product sums over one axis of a tensor, its gradients over the other.
  *   X      [rows][cols] of type xtype; offs == NULL: `batch` >= 1 such matrices [batch][rows][cols]
  *   Q, S   along the rows: containers of `rows` rows, axis cols (NULL, both, to skip)
  *   Qt, St along the columns: containers of `cols` rows, axis rows (NULL, both, to skip)
@@ -393,8 +394,9 @@ int hq_mx4_quantize(int32_t xtype, const void *X, int32_t rows, int32_t cols, in
 int hq_mx4_quantize_sr(int32_t xtype, const void *X, int32_t rows, int32_t cols, int32_t batch, const int32_t *offs,
                        uint64_t seed, uint8_t *Q, uint8_t *S, uint8_t *Qt, uint8_t *St, void *stream);
 
-/* The values of containers of `rows` rows and axis n, rounded to xtype once (exact but for overflow in HQ_FP16 and
- * for values below the type's smallest):
+/* The values of containers of `rows` rows and axis n, rounded to xtype once (exact but for magnitudes below the type's smallest, and above its
+ * largest, which become infinite: in HQ_FP16, and in the others 4 and 6 under a scale of 2^126, 2 and more under 2^127, which only magnitudes above
+ * 1.5 * 2^127, rounded up stochastically, come to):
  *   offs == NULL: `batch` >= 1 containers -> X [batch][rows][n]
  *   otherwise     one matrix of `batch` ragged segments along the axis -> X [rows][n]              */
 int hq_mx4_dequantize(const uint8_t *Q, const uint8_t *S, int32_t rows, int32_t n, int32_t batch, const int32_t *offs,

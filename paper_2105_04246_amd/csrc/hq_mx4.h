@@ -29,7 +29,7 @@ template <typename Launch> inline int hq_mx4_launch(unsigned blocks, unsigned th
 }
 
 // ---- real values -------------------------------------------------------------------------------
-// Rounded to nearest even where the type is narrower than fp32 (bf16, fp16: 2^-9 and 2^-12 relative at most).
+// Rounded to nearest even where the type is narrower than fp32 (half a step at most: bf16 2^-8, fp16 2^-11 relative).
 template <int TYPE> struct HqReal;
 template <> struct HqReal<HQ_FP32> {
     typedef float T;

@@ -70,12 +70,13 @@ template <int TYPE, int COUNT> __device__ inline void store_run(void *dst, const
 // from memory into one of two LDS buffers.  A step is half a chunk: one of a lane's two blocks of a row.  Tiles of 256 have 8 wavefronts of 64 x 128
 // (128 accumulator registers a lane, one workgroup to a compute unit), which read 192 KB of fragments a stage from LDS; tiles of 128 (4 wavefronts,
 // two workgroups) and of 64 (2 wavefronts, four) fill the card where there are few.
-// Measured: 8192 x 4096 x 4096 to bf16 65 us, 4.2 PFLOP/s (tiles of 128 86, of 64 121); the matrix pipes are busy for 46 % of the cycles at 2.07
-// GHz.  On a card where it took 70 us, it took 62 without its loads, 60 without its stores, 48 without loads and products: what is left is the start
-// of a tile (two of them to a compute unit) and its stores, during which all compute units do the same.  Slower (against 66 to 74 of the same day):
+// Measured: 8192 x 4096 x 4096 to bf16 64 us, 4.3 PFLOP/s (tiles of 128 86, of 64 121); the matrix pipes are busy for 46 % of the cycles at 2.07
+// GHz, and for 21 % of them a compute unit has no wavefront.  Beside 66.5 us of the same run: without stores 60, without loads 59, without both 49;
+// loads alone 38 (570 MB through L2), stores alone 14, none of the three 4.  (Codes of 0, which leave the clock higher: 54 us for 63.)  What holds it
+// up is that the three overlap in part only: a compute unit has one workgroup, and two tiles, one after the other.  Slower (against 66 to 74 of the same day):
 // stages of half a chunk in a ring of four 87 us, one buffer and four workgroups of 128 x 128 102, workgroups that keep their place and request the
-// next tile's stages before they store 77, lines touched ahead of their loads 73.
-// Weight gradients of 16 experts, 4096 x 1024 fp32 over 16384 rows: 63 us, 268 MB written and 60 MB read from memory (5.2 TB/s, a copy's rate).
+// next tile's stages before they store 77 (with spilled registers), lines touched ahead of their loads 73.
+// Weight gradients of 16 experts, 4096 x 1024 fp32 over 16384 rows: 63 to 65 us, 268 MB written and 60 MB read from memory (5.2 TB/s, a copy's rate).
 // ---------------------------------------------------------------------------------------
 
 // What the 16-byte blocks of an LDS row are XORed with.  Rows 2 k and 2 k + 1 take the two halves of the banks, the eight values of k all eight places of a
@@ -292,7 +293,8 @@ __global__ __launch_bounds__(64 * WM * WN) void mx4_tile_kernel(const ProductArg
 // Few rows: the bytes of B and latency count.  A workgroup takes 16 rows of B (of one expert) and all rows of A that meet them, 16 * MT at a time;
 // its wavefronts share the chunks between them and are added in LDS, in order.  Fragments come straight from memory, a lane 32 bytes of a row: the
 // rows of a chunk follow each other, so a wavefront reads runs of 2 KB.
-// Measured: 1 row, 4096 x 4096 3.7 us (8.9 MB of B: 2.4 TB/s, of which 2 us are an empty launch's); 16 rows, 32 experts of 2048 x 1024 5.1 us (3.5 TB/s).
+// Measured: 1 row, 4096 x 4096 3.7 to 4.0 us (8.9 MB of B: 2.2 TB/s and more, of which 2 us are an empty launch's); 16 rows, 32 experts of 2048 x 1024
+// 5.0 us (3.5 TB/s).
 // ---------------------------------------------------------------------------------------
 template <int MT, int GROUP> __global__ __launch_bounds__(512) void mx4_row_kernel(const ProductArgs a)
 {
@@ -404,6 +406,21 @@ int tiles_of(long n, int side) { return (int)((n + side - 1) / side); }
 // products to bf16 in tiles of 64, 128, 256: 256 x 4096 x 4096 11.3 / 10.5, 15.6 / 15.3, 20 / 22; 1024 x 4096 x 4096 18.3 / 16.7, 16.9 / 17.0,
 // 24.3 / 23.2; 2048 x 4096 x 4096 34 / 33, 27.9 / 24.7, 30.0 / 25.7; 4096 x 4096 x 4096 65 / 62, 53 / 48, 43 / 36; 1024 x 1024 x 16384 four ways
 // 25.4 / 23.3, 23.9 / 24.1, 31.3 / 30.3, one way 37 / 43, 54 / 60, 72 / 85.
+// It adds the outputs' time to that of stages which run beside them, so it says too much where outputs are many (8192 x 4096 x 4096 83 / 64; weight gradients
+// of 16 experts, 4096 x 1024 over 16384 rows, 92 / 63) and leans to smaller tiles there.  By expert, tiles of 64, 128, 256, us (*: what it takes;
+// products: rows x outputs of a row x contraction):
+//   products, 8 experts:  512 x 4096 x 1024    9.4*  9.9  10.7      products, 8 experts:   1024 x 1024 x 1024   6.1*  6.9   9.5
+//                        1024                 13.3  11.6* 11.0                             4096                10.7   9.7* 10.2
+//                        2048                 17.6  15.0* 13.8                             8192                15.7  15.0* 11.2
+//                        4096                 28.0  22.2  22.3*                            8192 x 1024 x 4096  36.9  35.5* 24.7
+//                        8192                 45.9  35.6  33.8*     products, 32 experts:  4096 x 1024 x 4096  30.7  27.4* 26.5
+//                       16384                 84.3  62.9  56.7*                           16384 x 1024 x 1024  27.2  22.4  22.8*
+//   weight gradients:  4096 x 1024, 16384 rows, 16 experts  96.9  76.2  71.1*      1024 x 1024, 8192 rows, 4 experts  10.7  12.4* 15.8
+//                      4096 x 1024,  8192 rows, 16 experts  67.4  56.9  58.5*       512 x 512, 16384 rows, 8 experts  10.5* 10.2  14.9
+//                      2048 x 1024, 16384 rows,  4 experts  34.6  25.6* 28.8        512 x 512,  4096 rows, 8 experts   5.5*  5.8   8.5
+//                      1024 x 1024, 16384 rows,  8 experts  22.1  19.3* 19.4        256 x 512,  4096 rows, 4 experts   5.6*  7.1  10.5
+//   split 1, 2, 4, 8 ways:  512 x 1024, 16384 rows, 2 experts  tiles of 64 19.8 17.9 17.5 24.8, of 128 28.0 20.8 18.2* 22.6
+//                           256 x 512,  16384 rows, 2 experts  tiles of 64 18.2 13.9 12.0 12.9*, of 128 27.4 18.9 14.6 13.7
 double estimate(int side, int splits, double tiles, double stages, double outputs, double bytes)
 {
     const double n = tiles * splits;
@@ -416,6 +433,8 @@ Plan plan_of(const hq_mx4_problem *p, int group)
     // Few rows: B is read once and the rows of A beside it, without LDS.  (Rows / tiles of 64, us: one product of K = 4096, N = 4096 16 rows
     // 4.3 / 9, 32 rows 5.3 / 8.5, 64 rows 9.2 / 9.1.  By expert the count is known on the device only, its mean here: 64 experts of 4096 x 1024
     // 128 rows 21.1 / 26.3, 512 rows 32.5 / 29.9; 8 experts of 1024 x 4096 32 rows 5.9 / 10.3, 128 rows 12.5 / 10.5; 2 experts 32 rows 5.1 / 10.4.)
+    // A mean says nothing of the routing.  Just below and at the line, all rows with one expert (evenly): 64 experts of 4096 x 1024 39 / 25 (32 / 30);
+    // 8 of 1024 x 4096 12.1 / 10.6 (5.7 / 10.5); 256 of 2048 x 1024 155 / 55 (66 / 75); 4096 of 256 x 512 2100 / 514 (69 / 493), its rows 16 at a time.
     const long experts = p->experts;
     if (group == BY_ROWS && p->M < 8 * experts) return Plan{1, 1};
     if (group != BY_CHUNKS && p->M <= 32) return Plan{p->M <= 16 ? 1 : 2, 1};

@@ -3,16 +3,18 @@
 //   block of 32 values x along an axis:  byte = max(exponent field of max |x| - 2 [+ 1 if its mantissa > 1.5: stochastic], 0)
 //   t = |x| 2^(127 - byte), exact in fp32; code = t to nearest even on the grid 0 .. 6, or up with probability of t's share of its step
 //
-// Bound by HBM: 4 or 2 bytes read per value, 17/32 of a byte written per direction; stochastic rounding by the vector pipes (a draw's three
-// multiplications, two roundings).
+// Bound by HBM: 4 or 2 bytes read per value, 17/32 of a byte written per direction; stochastic rounding by the vector pipes (a draw's four integer
+// multiplications at a quarter of the rate, one of them the term of the index's high word, made for every value; a rounding per direction).
 // Each direction by workgroups of its own, in small pieces: along the rows 4 rows of 256 columns a wavefront, four columns a lane (a
 // block lies in eight neighbouring lanes: three DPP steps find its maximum), along the columns 32 rows of 64 columns, a column a lane, whose block is
 // the lane's own.  Eight wavefronts make the 256 rows of a chunk along the columns; its codes are put together in LDS, so that the container is
 // written in whole 128-byte lines.  Large tensors, to nearest: both directions from one reading, 32 rows of 256 columns a wavefront
-// whose values stay in registers.
+// whose values stay in registers (fp32: all 256 of a lane, and one is spilled).
 // Measured, both directions (pieces / one reading, us): fp32 512 x 512 3.6 / 8.5, 2048 x 2048 5.0 / 9.3, 4096 x 2048 12.6 / 11.3, 16384 x 4096
 // 88 / 75.5; bf16 4096 x 2048 7.9 / 10.1, 4096 x 4096 15.1 / 12.8, 16384 x 4096 52.7 / 49.2 (4.2 TB/s).  Stochastic: pieces throughout,
-// fp32 512 x 512 5.8 / 26, 16384 x 4096 134 / 157.
+// fp32 512 x 512 5.8 / 26, 16384 x 4096 128 / 157.
+// One direction alone, pieces (16384 x 4096, along the rows / along the columns, us; the input partly in the last-level cache from the call before):
+// fp32 45 / 47.5, bf16 29 / 26.
 #include "hq_internal.h"
 #include "hq_mx4.h"
 
